@@ -357,6 +357,72 @@ size_t a3_first_token_workspace_bytes(const a3_handle* h);
 int a3_first_token(const a3_handle* h, const void* x_row, const void* final_norm, const void* lm_head, int vocab,
                    float* logits_out, int32_t* token_out, void* ws, size_t ws_bytes, a3_stream stream);
 
+/* ---- decoding on paged caches -------------------------------------------------------------------------------- */
+
+/* One layer's cache in pages that sequences share: page p of the keys at k_pages + p*page_stride bytes, laid out
+ * [page_size][Hkv][D] as every cache here is, of the values likewise.  So a fused layer whose slots are a multiple of page_size is
+ * a pool of pages as it stands.  Held in bf16, or in 8 bits (e4m3) with one fp32 scale per KV head: stored value x scale.
+ * A sequence owns row s of a page table [n_seqs][max_pages] (dev, int32): its slot t is entry t % page_size of page
+ * table[s][t / page_size].  Entries behind a sequence's last page are never read. */
+#define A3_CACHE_BF16 0
+#define A3_CACHE_E4M3 1
+typedef struct {
+  void* k_pages;        /* dev, 16-byte aligned */
+  void* v_pages;
+  uint64_t page_stride; /* bytes, a multiple of 16: K and V pages may lie interleaved in one pool */
+  int32_t n_pages, page_size;
+  int32_t type;         /* A3_CACHE_BF16 or A3_CACHE_E4M3 */
+  int32_t reserved;
+  const float* k_scale; /* dev [Hkv], A3_CACHE_E4M3 only */
+  const float* v_scale;
+} a3_paged_cache;
+
+/* Rows into a paged cache, rotated on the way: row r goes to slot row_slot[r] of sequence row_seq[r],
+ *   k' = R(pos) k_rows[r], v' = v_rows[r], q_out[r] = R(pos) q_rows[r],   pos = row_pos ? row_pos[r] : row_slot[r]
+ * in fp32 arithmetic, rounded once to the type that is stored (e4m3: k'/k_scale[head], beyond +-448 the largest value; NaN stays NaN).
+ * pos may be negative (turns back) and differs from the slot in a cache that a3_evict_layer has shortened, or
+ * where a stored chunk's keys at local positions are recovered (Eq. 2: pos = the chunk's offset for every row).  rotate = 0: keys and
+ * queries are copied as they are (rows of a fused cache).  q_rows and q_out: both NULL where there are no queries to rotate; q_out may be
+ * q_rows.  Strides between rows in elements, multiples of 8: q, k and v may be columns of one buffer; each row is
+ * [heads][D] without gaps.  row_seq[r] < 0 marks padding: nothing of such a row is written.  A row whose sequence, slot, page or
+ * |pos| is out of range (n_seqs, max_pages, n_pages, max_positions) is left out as a whole and A3_DEV_BAD_POSITION is set.  Rows of
+ * one call must go to different slots.  One launch. */
+int a3_paged_append(const a3_handle* h, const a3_paged_cache* cache, const int32_t* page_table, int n_seqs, int max_pages,
+                    const int32_t* row_seq, const int32_t* row_slot, const int32_t* row_pos, int rotate, const void* q_rows,
+                    size_t q_stride, const void* k_rows, size_t k_stride, const void* v_rows, size_t v_stride, int M, void* q_out,
+                    size_t q_out_stride, a3_stream stream);
+
+/* Attention of one new token per sequence over its pages:
+ *   out[s][h] = sum over t < cache_len[s] of Softmax_t(scale * q[s][h] . k[s][t][h/G]) v[s][t][h/G],  G = Hq/Hkv
+ * q_rows: dev [n_seqs][Hq][D] bf16, rotated, q_stride elements (a multiple of 8) between sequences; cache_len: dev [n_seqs], the new
+ * token's own slot included; out: dev [n_seqs][Hq][D] bf16; lse_out: dev [n_seqs][Hq] fp32 natural-log row log-sum-exps of the scaled
+ * logits, or NULL.  A sequence of length 0 (padding of a batch of fixed size) gives zeros and -inf.  A length below 0 or above
+ * max_pages*page_size counts as 0, keys and values of a page outside [0, n_pages) count as zeros, and both set A3_DEV_BAD_POSITION.
+ * Lengths are read on the device only, so a captured call follows them.  The result is deterministic.
+ * ws: dev, 256-byte aligned, a3_paged_attention_workspace_bytes(h) bytes, borrowed until the call's kernels have ended; needs
+ * no clearing.  Two launches, no allocation, no synchronisation. */
+size_t a3_paged_attention_workspace_bytes(const a3_handle* h);
+int a3_paged_attention(const a3_handle* h, const a3_paged_cache* cache, const int32_t* page_table, int n_seqs, int max_pages,
+                       const int32_t* cache_len, const void* q_rows, size_t q_stride, float scale, void* out, float* lse_out, void* ws,
+                       size_t ws_bytes, a3_stream stream);
+
+/* Log probabilities of given tokens, entropies and the best alternatives, from rows of logits (a3_first_token's, or a projection of
+ * many rows): with lse = log sum_i exp(x_i),
+ *   logprob_out[m] = x[targets[m]] - lse,   entropy_out[m] = -sum_i p_i log p_i (natural logarithm; p_i = 0 adds nothing),
+ *   top_ids_out[m][j], top_logprobs_out[m][j]: the n_top largest in descending order, ties to the lower id.
+ * logits: dev [M][vocab] of `type`, row_stride elements between rows, no alignment beyond the element's.  targets: dev [M]
+ * int32 or NULL (then no logprob_out); a negative target (padding) gives 0, one beyond the vocabulary NaN and
+ * A3_DEV_BAD_POSITION.  -inf logits (tokens ruled out) are ordinary values.  A row with a NaN or +inf, or with nothing but -inf, has no
+ * distribution: its log probabilities and entropy are NaN and A3_DEV_NONFINITE_SCORE is set; NaNs come last among the alternatives.
+ * logprob_out and entropy_out: dev [M] fp32 or NULL; top_*_out: dev [M][n_top], NULL iff n_top = 0; n_top <= A3_LOGPROBS_MAX_TOP and
+ * n_top <= vocab.  One launch, no workspace. */
+#define A3_LOGPROBS_MAX_TOP 32
+#define A3_LOGITS_FP32 0
+#define A3_LOGITS_BF16 1
+#define A3_LOGITS_FP16 2
+int a3_token_logprobs(const a3_handle* h, const void* logits, int type, size_t row_stride, int M, int vocab, const int32_t* targets,
+                      int n_top, float* logprob_out, float* entropy_out, int32_t* top_ids_out, float* top_logprobs_out, a3_stream stream);
+
 /* Waits for `stream`, reads and clears the device status word (A3_DEV_* bits). */
 int a3_device_status(const a3_handle* h, uint32_t* bits_out, a3_stream stream);
 const char* a3_status_string(int status);

@@ -63,6 +63,11 @@ class HostIO(C.Structure):
                 ("x0", C.c_void_p), ("rows_out", C.c_void_p), ("x_out", C.c_void_p)]
 
 
+class PagedCacheDesc(C.Structure):
+    _fields_ = [("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("page_stride", C.c_uint64), ("n_pages", C.c_int32),
+                ("page_size", C.c_int32), ("type", C.c_int32), ("reserved", C.c_int32), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
 # a3_option (include/a3.h)
 (OPT_ATTN_SPLIT, OPT_ATTN_PAIR, OPT_ATTN_MAX_CTAS, OPT_SWIGLU_NARROW, OPT_SWIGLU_PAIR, OPT_RESIDUAL_T, OPT_GEMM_BN_RESIDUAL,
  OPT_GEMM_BN_SWIGLU, OPT_GEMM_BN_QKV, OPT_GEMM_STAGES_RESIDUAL, OPT_GEMM_STAGES_SWIGLU, OPT_GEMM_STAGES_QKV,
@@ -71,7 +76,8 @@ class HostIO(C.Structure):
 EXPORTS = ("a3_create", "a3_destroy", "a3_set_option", "a3_scores_workspace_bytes", "a3_swiglu_rows", "a3_layer_workspace_bytes", "a3_request_workspace_bytes", "a3_host_staging_bytes",
            "a3_recompute_count", "a3_rope_rerotate", "a3_query_scores", "a3_query_scores_static", "a3_topk_select", "a3_recompute_layer",
            "a3_scatter_kv", "a3_gather_rows", "a3_precompute_chunk", "a3_first_token_workspace_bytes", "a3_first_token",
-           "a3_evict_count", "a3_evict_workspace_bytes", "a3_evict_layer", "a3_chunk_edge_rows", "a3_random_rows", "a3_fuse_request", "a3_fuse_batch", "a3_fuse_request_host",
+           "a3_evict_count", "a3_evict_workspace_bytes", "a3_evict_layer", "a3_paged_append", "a3_paged_attention_workspace_bytes",
+           "a3_paged_attention", "a3_token_logprobs", "a3_chunk_edge_rows", "a3_random_rows", "a3_fuse_request", "a3_fuse_batch", "a3_fuse_request_host",
            "a3_graph_capture", "a3_graph_launch", "a3_graph_kernel_count", "a3_graph_destroy",
            "a3_device_status", "a3_status_string", "a3_last_cuda_error", "a3_launch_count", "a3_profile_enable",
            "a3_profile_read", "a3_kernel_class_name", "a3_plan_layer")
@@ -123,6 +129,11 @@ def _load():
     lib.a3_first_token_workspace_bytes.argtypes = [vp]
     lib.a3_first_token_workspace_bytes.restype = sz
     lib.a3_first_token.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, sz, vp]
+    lib.a3_paged_append.argtypes = [vp, C.POINTER(PagedCacheDesc), vp, i32, i32, vp, vp, vp, i32, vp, sz, vp, sz, vp, sz, i32, vp, sz, vp]
+    lib.a3_paged_attention_workspace_bytes.argtypes = [vp]
+    lib.a3_paged_attention_workspace_bytes.restype = sz
+    lib.a3_paged_attention.argtypes = [vp, C.POINTER(PagedCacheDesc), vp, i32, i32, vp, vp, sz, C.c_float, vp, vp, vp, sz, vp]
+    lib.a3_token_logprobs.argtypes = [vp, vp, i32, sz, i32, i32, vp, i32, vp, vp, vp, vp, vp]
     lib.a3_fuse_request.argtypes = [vp, C.POINTER(Request), vp, sz, vp]
     lib.a3_fuse_batch.argtypes = [vp, C.POINTER(Request), i32, vp, sz, vp]
     lib.a3_fuse_request_host.argtypes = [vp, C.POINTER(Request), C.POINTER(HostIO), vp, sz, vp, sz, vp]
@@ -243,6 +254,40 @@ def plan_layer(shape, rows: int, sm_count: int = 148) -> Dict[str, int]:
     plan = LayerPlan()
     _check(_load().a3_plan_layer(C.byref(desc), int(sm_count), int(rows), C.byref(plan)), "a3_plan_layer")
     return {n: int(getattr(plan, n)) for n, _ in LayerPlan._fields_}
+
+
+def _need(ok: bool, where: str):
+    """Refuses, as the library does, what only the binding can see of a tensor: its type, shape, strides and device."""
+    if not ok:
+        raise A3Error(-1, where)
+
+
+class PagedCache:
+    """One layer's paged cache (a3_paged_cache): k_pages and v_pages [n_pages][page_size][Hkv][D], bf16, or float8_e4m3fn with one fp32
+    scale per KV head each.  A page is contiguous; pages may be apart (both pools alike).  Keeps the tensors alive."""
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+                 v_scale: Optional[torch.Tensor] = None):
+        where = "PagedCache"
+        _need(k_pages.dim() == 4 and k_pages.shape == v_pages.shape and k_pages.stride() == v_pages.stride()
+              and k_pages.dtype == v_pages.dtype and k_pages.device == v_pages.device and min(k_pages.shape) > 0, where + " pages")
+        n, size, heads, d = k_pages.shape
+        _need(k_pages.stride()[1:] == (heads * d, d, 1), where + " pages are contiguous")
+        _need(k_pages.dtype in (torch.bfloat16, torch.float8_e4m3fn), where + " type")
+        packed = k_pages.dtype == torch.float8_e4m3fn
+        for s in (k_scale, v_scale):
+            _need((s is not None) == packed, where + " scales come with 8 bits")
+            _need(s is None or (s.dtype == torch.float32 and s.shape == (heads,) and s.is_contiguous() and s.device == k_pages.device),
+                  where + " scales")
+        self.k_pages, self.v_pages, self.k_scale, self.v_scale = k_pages, v_pages, k_scale, v_scale
+        self.page_size, self.n_kv_heads, self.head_dim, self.device = size, heads, d, k_pages.device
+        stride = k_pages.stride(0) if n > 1 else size * heads * d
+        self.desc = PagedCacheDesc(k_pages.data_ptr(), v_pages.data_ptr(), stride * k_pages.element_size(), n, size, 1 if packed else 0, 0,
+                                   _ptr(k_scale), _ptr(v_scale))
+        self._ref = C.byref(self.desc)
+
+
+_LOGIT_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
 class A3:
@@ -397,6 +442,86 @@ class A3:
         _check(_load().a3_first_token(self._h, _ptr(x_row), _ptr(final_norm), _ptr(lm_head), vocab, _ptr(logits), _ptr(token),
                                       _ptr(ws), ws.numel(), _stream()), "a3_first_token")
         return logits, token
+
+    # ---- decoding on paged caches
+    def _indices(self, where, *tensors):
+        for t in tensors:
+            _need(t.dtype == torch.int32 and t.device == self.device and t.is_contiguous(), where + ": int32 indices on the engine's device")
+
+    def _rows(self, where, t, heads, n):
+        """Elements between the rows of t [n][heads][D], whose heads lie next to each other."""
+        m = self.shape
+        _need(t.dtype == torch.bfloat16 and t.shape == (n, heads, m.head_dim) and t.device == self.device, where)
+        sr, sh, se = t.stride()
+        _need(n == 0 or (se == 1 and (sh == m.head_dim or heads == 1)), where)
+        return sr if n > 1 else heads * m.head_dim
+
+    def _paged(self, where, cache, page_table):
+        m = self.shape
+        _need(cache.n_kv_heads == m.n_kv_heads and cache.head_dim == m.head_dim and cache.device == self.device, where + ": the cache is another model's")
+        self._indices(where, page_table)
+        _need(page_table.dim() == 2, where + ": page table")
+
+    def paged_append(self, cache: PagedCache, page_table, row_seq, row_slot, k_rows, v_rows, q_rows=None, row_pos=None, rotate=True, q_out=None):
+        """a3_paged_append; page_table [n_seqs][max_pages], rows [M][heads][D] (columns of a wider buffer will do); returns q_out or None."""
+        where, m, M = "a3_paged_append", self.shape, row_seq.shape[0]
+        self._paged(where, cache, page_table)
+        self._indices(where, row_seq, row_slot, *(() if row_pos is None else (row_pos,)))
+        _need(row_seq.shape == row_slot.shape == (M,) and (row_pos is None or row_pos.shape == (M,)), where + ": rows")
+        ks, vs = self._rows(where + ": k_rows", k_rows, m.n_kv_heads, M), self._rows(where + ": v_rows", v_rows, m.n_kv_heads, M)
+        qs = os = 0
+        if q_rows is not None:
+            qs = self._rows(where + ": q_rows", q_rows, m.n_q_heads, M)
+            if q_out is None:
+                q_out = torch.empty((M, m.n_q_heads, m.head_dim), dtype=torch.bfloat16, device=self.device)
+            os = self._rows(where + ": q_out", q_out, m.n_q_heads, M)
+        _need(q_rows is not None or q_out is None, where + ": q_out without q_rows")
+        _check(_load().a3_paged_append(self._h, cache._ref, page_table.data_ptr(), page_table.shape[0], page_table.shape[1], row_seq.data_ptr(),
+                                       row_slot.data_ptr(), None if row_pos is None else row_pos.data_ptr(), 1 if rotate else 0,
+                                       None if q_rows is None else q_rows.data_ptr(), qs, k_rows.data_ptr(), ks, v_rows.data_ptr(), vs, M,
+                                       None if q_out is None else q_out.data_ptr(), os, _stream()), where)
+        return q_out
+
+    def paged_attention(self, cache: PagedCache, page_table, cache_len, q_rows, scale=None, out=None, want_lse=False):
+        """a3_paged_attention; returns (out [n_seqs][Hq][D], lse [n_seqs][Hq] or None).  The workspace is allocated by torch for
+        this call alone, so that calls on several streams, or captured into several graphs, share none."""
+        where, m, n = "a3_paged_attention", self.shape, cache_len.shape[0]
+        lib = _load()
+        self._paged(where, cache, page_table)
+        self._indices(where, cache_len)
+        _need(cache_len.dim() == 1 and page_table.shape[0] == n, where + ": sequences")
+        qs = self._rows(where + ": q_rows", q_rows, m.n_q_heads, n)
+        if out is None:
+            out = torch.empty((n, m.n_q_heads, m.head_dim), dtype=torch.bfloat16, device=self.device)
+        _need(out.dtype == torch.bfloat16 and out.shape == (n, m.n_q_heads, m.head_dim) and out.is_contiguous() and out.device == self.device, where + ": out")
+        lse = torch.empty((n, m.n_q_heads), dtype=torch.float32, device=self.device) if want_lse else None
+        nbytes = lib.a3_paged_attention_workspace_bytes(self._h)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        _check(lib.a3_paged_attention(self._h, cache._ref, page_table.data_ptr(), n, page_table.shape[1], cache_len.data_ptr(), q_rows.data_ptr(), qs,
+                                      m.head_dim ** -0.5 if scale is None else scale, out.data_ptr(), None if lse is None else lse.data_ptr(),
+                                      ws.data_ptr(), nbytes, _stream()), where)
+        return out, lse
+
+    def token_logprobs(self, logits, targets=None, n_top=0):
+        """a3_token_logprobs on logits [M][vocab] (fp32, bf16 or fp16; rows may be apart); returns (logprob [M] or None without targets,
+        entropy [M], top_ids [M][n_top] and top_logprobs [M][n_top], or None)."""
+        where = "a3_token_logprobs"
+        _need(logits.dim() == 2 and logits.dtype in _LOGIT_TYPES and logits.device == self.device, where + ": logits")
+        M, vocab = logits.shape
+        _need(vocab > 0 and (logits.stride(1) == 1 or vocab == 1), where + ": logits of a row lie next to each other")
+        dev, logprob, ids, lps = self.device, None, None, None
+        if targets is not None:
+            self._indices(where, targets)
+            _need(targets.shape == (M,), where + ": targets")
+            logprob = torch.empty(M, dtype=torch.float32, device=dev)
+        entropy = torch.empty(M, dtype=torch.float32, device=dev)
+        if n_top > 0:
+            ids, lps = torch.empty((M, n_top), dtype=torch.int32, device=dev), torch.empty((M, n_top), dtype=torch.float32, device=dev)
+        _check(_load().a3_token_logprobs(self._h, logits.data_ptr(), _LOGIT_TYPES[logits.dtype], logits.stride(0) if M > 1 else vocab, M, vocab,
+                                         None if targets is None else targets.data_ptr(), n_top, None if logprob is None else logprob.data_ptr(),
+                                         entropy.data_ptr(), None if ids is None else ids.data_ptr(), None if lps is None else lps.data_ptr(),
+                                         _stream()), where)
+        return logprob, entropy, ids, lps
 
     def make_request(self, chunks, n_chunks, max_chunk_len, n_ctx, n_question, x0, k_fused, v_fused, ratio=0.15,
                      select_layer=1, n_system=0, forced_re=None, n_recompute=None, score_source=0, evict_capacity=0,

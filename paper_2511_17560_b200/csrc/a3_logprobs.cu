@@ -1,0 +1,381 @@
+// Log probabilities of given tokens, entropy and the best alternatives (a3_token_logprobs), from rows of logits.
+//
+//   M = max x,  s = sum exp(x - M),  w = sum exp(x - M) (x - M)
+//   logprob = x_t - M - log s,   entropy = log s - w / s
+//
+// The logits are read once: bound by HBM where rows are many, by latency where they are few.  A row belongs to one CTA or, where rows
+// are fewer than the device holds, to a cluster whose CTAs join their parts through distributed shared memory.  Each thread keeps the
+// running (M, s, w) of its own elements.  s is carried without the 1 of one largest element and ends in log1p: where one token
+// has nearly all of the probability, what it lacks of 1 and the entropy come from the other tokens alone.
+//
+// The alternatives come from the same pass: the n-th largest of the threads' maxima is a bound that at least n elements reach, and only
+// the threads whose own maximum reaches it - little more than n of 512 - are gone through again (from L2), a warp together on one
+// thread's elements.  What reaches the bound, usually 1-2 n elements, is ranked by counting.
+#include <cooperative_groups.h>
+#include <cuda_fp16.h>
+
+#include "a3_internal.cuh"
+
+namespace a3 {
+
+constexpr int LP_THREADS = 512, LP_WARPS = LP_THREADS / 32, LP_U = 4, LP_CAP = 1024, LP_TOP = A3_LOGPROBS_MAX_TOP;
+constexpr float LOG2E = 1.44269504088896341f;
+constexpr float LP_FAR = -200.f;  // exp of it is 0 in fp32, and unlike that of -inf or of the lowest value its product with that 0 is 0 too
+
+struct LogprobArgs {
+  const void* logits;
+  long long row_stride;
+  int M, vocab;
+  const int32_t* targets;
+  int n_top;
+  float *logprob, *entropy;
+  int32_t* top_ids;
+  float* top_logprobs;
+  uint32_t* status;
+};
+
+template <typename T>
+struct Logit;
+template <>
+struct Logit<float> {
+  static constexpr int VE = 4;
+  __device__ static void unpack(const uint4& v, float* f) { f[0] = __uint_as_float(v.x), f[1] = __uint_as_float(v.y), f[2] = __uint_as_float(v.z), f[3] = __uint_as_float(v.w); }
+  __device__ static float one(const float* p) { return *p; }
+};
+template <>
+struct Logit<bf16> {
+  static constexpr int VE = 8;
+  __device__ static void unpack(const uint4& v, float* f) { unpack8(v, f); }
+  __device__ static float one(const bf16* p) { return __bfloat162float(*p); }
+};
+template <>
+struct Logit<__half> {
+  static constexpr int VE = 8;
+  __device__ static void unpack(const uint4& v, float* f) {
+    const __half2* p = reinterpret_cast<const __half2*>(&v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 t = __half22float2(p[i]);
+      f[2 * i] = t.x, f[2 * i + 1] = t.y;
+    }
+  }
+  __device__ static float one(const __half* p) { return __half2float(*p); }
+};
+
+__device__ __forceinline__ float lp_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+// Whole numbers in the order of the values: NaN 0, -inf LP_NONE; both zeros alike.
+constexpr uint32_t LP_NONE = 0x007fffffu;
+__device__ __forceinline__ uint32_t ordered(float x) {
+  const uint32_t u = __float_as_uint(x + 0.f);
+  return x != x ? 0u : u ^ ((int32_t)u < 0 ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ float unordered(uint32_t k) { return k == 0 ? NAN : __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xffffffffu)); }
+// larger is better: the value, then the lower id
+__device__ __forceinline__ unsigned long long lp_key(uint32_t o, int id) { return (unsigned long long)o << 32 | (0xffffffffu - (uint32_t)id); }
+__device__ __forceinline__ int key_id(unsigned long long k) { return (int)(0xffffffffu - (uint32_t)k); }
+
+struct LpStats {
+  float m, s, w;  // s without the 1 of one largest element
+};
+__device__ __forceinline__ float warp_sum(float x) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(LP_THREADS, 2)
+logprobs_kernel(const LogprobArgs a) {
+  namespace cg = cooperative_groups;
+  constexpr int VE = Logit<T>::VE;
+  __shared__ LpStats s_stats;
+  __shared__ float s_red[3][LP_WARPS];
+  __shared__ unsigned long long s_cand[LP_CAP], s_top[LP_TOP], s_best[LP_WARPS];
+  __shared__ int s_count, s_holder;
+  pdl_wait();
+  pdl_launch_dependents();
+  cg::cluster_group cluster = cg::this_cluster();
+  const int parts = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const int row = blockIdx.x / parts, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const T* x = reinterpret_cast<const T*>(a.logits) + row * a.row_stride;
+  // 16-byte vectors from the first boundary on, the few elements before and behind them one by one
+  const int head = min(a.vocab, (int)((16 - ((uintptr_t)x & 15)) % 16 / sizeof(T)));
+  const int n_vec = (a.vocab - head) / VE, tail0 = head + n_vec * VE;
+  const int v0 = (int)((long long)n_vec * rank / parts), v1 = (int)((long long)n_vec * (rank + 1) / parts);
+  const uint4* xv = reinterpret_cast<const uint4*>(x + head);
+  // this thread's single element: of the head in the first CTA, of the tail in the last
+  int single = -1;
+  if (rank == 0 && tid < head) single = tid;
+  if (rank == parts - 1 && tid >= 32 && tid - 32 < a.vocab - tail0) single = tail0 + tid - 32;
+
+  float m = -INFINITY, s = 0.f, w = 0.f;
+  auto take = [&](const float* f, int n) {
+    float most = f[0];
+#pragma unroll
+    for (int i = 1; i < n; ++i) most = fmaxf(most, f[i]);  // of the numbers
+    if (most > m) {
+      if (m > -INFINITY) {
+        const float d = fmaxf(m - most, LP_FAR), g = lp_ex2(d * LOG2E);
+        w = g * (w + s * d);
+        s *= g;
+      }
+      m = most;
+    }
+    if (m > -INFINITY) {
+#pragma unroll
+      for (int i = 0; i < n; ++i) {
+        const float d = max_nan(f[i] - m, LP_FAR), e = lp_ex2(d * LOG2E);  // NaN goes into s
+        s += e;
+        w += e * d;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < n; ++i)
+        if (f[i] != f[i]) s = NAN;
+    }
+  };
+  for (int v = v0 + tid; v < v1; v += LP_THREADS * LP_U) {
+    uint4 raw[LP_U];
+    float f[LP_U * VE];
+#pragma unroll
+    for (int u = 0; u < LP_U; ++u)
+      if (v + u * LP_THREADS < v1) raw[u] = __ldg(xv + v + u * LP_THREADS);
+#pragma unroll
+    for (int u = 0; u < LP_U; ++u) {
+      if (v + u * LP_THREADS < v1) {
+        Logit<T>::unpack(raw[u], f);
+        take(f, VE);
+      }
+    }
+  }
+  const uint32_t mine = ordered(m);  // of the vectors alone; LP_NONE: nothing above -inf
+  if (single >= 0) {
+    const float f = Logit<T>::one(x + single);
+    take(&f, 1);
+  }
+
+  // ---- the CTA's statistics
+  if (tid == 0) s_count = 0, s_holder = LP_THREADS;
+  float most = m;
+#pragma unroll
+  for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+  if (lane == 0) s_red[0][warp] = most;
+  __syncthreads();
+  most = s_red[0][0];
+#pragma unroll
+  for (int i = 1; i < LP_WARPS; ++i) most = fmaxf(most, s_red[0][i]);
+  if (m == most) atomicMin(&s_holder, tid);
+  __syncthreads();
+  {
+    const float d = fmaxf(m - most, LP_FAR), g = m > -INFINITY ? lp_ex2(d * LOG2E) : 0.f;
+    float ps = g * (tid == s_holder ? s - 1.f : s), pw = m > -INFINITY ? g * (w + s * d) : 0.f;
+    ps = warp_sum(ps);
+    pw = warp_sum(pw);
+    if (lane == 0) s_red[1][warp] = ps, s_red[2][warp] = pw;
+  }
+  __syncthreads();
+  if (tid == 0) {
+    float ps = 0.f, pw = 0.f;
+    for (int i = 0; i < LP_WARPS; ++i) ps += s_red[1][i], pw += s_red[2][i];
+    s_stats = LpStats{most, ps, pw};
+  }
+
+  // ---- the CTA's best elements above -inf
+  if (a.n_top > 0) {
+    const int n = a.n_top;
+    // a bound that n threads' maxima reach (its upper 16 bits: a lower one does as well)
+    uint32_t bound = 0;
+#pragma unroll
+    for (int bit = 31; bit >= 16; --bit) {
+      const uint32_t c = bound | 1u << bit;
+      if (__syncthreads_count(mine >= c) >= n) bound = c;
+    }
+    if (bound <= LP_NONE) bound = LP_NONE + 1;
+    auto offer = [&](float f, int id) {
+      const uint32_t o = ordered(f);
+      if (o >= bound) {
+        const int at = atomicAdd(&s_count, 1);
+        if (at < LP_CAP) s_cand[at] = lp_key(o, id);
+      }
+    };
+    // one thread's elements, a warp together: `use(value, id)` for each
+    auto again = [&](int t, auto use) {
+      for (int v = v0 + t + lane * LP_THREADS; v < v1; v += 32 * LP_THREADS) {
+        float f[VE];
+        Logit<T>::unpack(__ldg(xv + v), f);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) use(f[e], head + v * VE + e);
+      }
+    };
+    for (uint32_t left = __ballot_sync(0xffffffffu, mine >= bound); left; left &= left - 1) again(warp * 32 + __ffs(left) - 1, offer);
+    if (single >= 0) offer(Logit<T>::one(x + single), single);
+    __syncthreads();
+    const int count = s_count;
+    if (tid < n) s_top[tid] = 0;
+    __syncthreads();
+    if (count <= LP_CAP) {
+      for (int i = tid; i < count; i += LP_THREADS) {
+        const unsigned long long k = s_cand[i];
+        int better = 0;
+        for (int j = 0; j < count; ++j) better += s_cand[j] > k;
+        if (better < n) s_top[better] = k;
+      }
+    } else {
+      // More elements at the bound than there is room for (a row of equal values): the best of all, n times, where each time only
+      // the thread that had it looks for its next.
+      unsigned long long best = 0, last = ~0ull;
+      auto next_of = [&](int t) {  // of thread t, below `last`
+        unsigned long long k = 0;
+        again(t, [&](float f, int id) {
+          const uint32_t o = ordered(f);
+          const unsigned long long c = o > LP_NONE ? lp_key(o, id) : 0;
+          if (c < last && c > k) k = c;
+        });
+#pragma unroll
+        for (int o = 16; o; o >>= 1) k = max(k, __shfl_xor_sync(0xffffffffu, k, o));
+        return k;
+      };
+      for (int t = 0; t < 32; ++t) {
+        const unsigned long long k = next_of(warp * 32 + t);
+        if (lane == t) best = k;
+      }
+      unsigned long long extra = 0;
+      if (single >= 0) {
+        const uint32_t o = ordered(Logit<T>::one(x + single));
+        extra = o > LP_NONE ? lp_key(o, single) : 0;
+      }
+      for (int i = 0; i < n; ++i) {
+        unsigned long long k = max(best, extra);
+#pragma unroll
+        for (int o = 16; o; o >>= 1) k = max(k, __shfl_xor_sync(0xffffffffu, k, o));
+        if (lane == 0) s_best[warp] = k;
+        __syncthreads();
+        for (int j = 0; j < LP_WARPS; ++j) k = max(k, s_best[j]);
+        if (tid == 0) s_top[i] = k;
+        last = k;
+        if (extra == k) extra = 0;
+        const uint32_t whose = __ballot_sync(0xffffffffu, best == k && k != 0);
+        if (whose) {
+          const int t = __ffs(whose) - 1;
+          const unsigned long long nk = next_of(warp * 32 + t);
+          if (lane == t) best = nk;
+        }
+        __syncthreads();
+      }
+    }
+  }
+
+  // ---- the parts of the row, joined by the first CTA
+  if (parts > 1) cluster.sync();
+  else __syncthreads();
+  if (rank == 0) {
+    LpStats all = s_stats;
+    if (parts > 1) {
+      for (int r = 1; r < parts; ++r) {
+        const LpStats o = *cluster.map_shared_rank(&s_stats, r);
+        if (o.m > all.m) {
+          const float d = fmaxf(all.m - o.m, LP_FAR), g = all.m > -INFINITY ? lp_ex2(d * LOG2E) : 0.f;
+          const float w1 = all.m > -INFINITY ? g * (all.w + (1.f + all.s) * d) : 0.f;
+          all = LpStats{o.m, o.s + g * (1.f + all.s), o.w + w1};
+        } else if (o.m > -INFINITY) {
+          const float d = fmaxf(o.m - all.m, LP_FAR), g = lp_ex2(d * LOG2E);
+          all.s += g * (1.f + o.s);
+          all.w += g * (o.w + (1.f + o.s) * d);
+        }
+        if (o.s != o.s) all.s = NAN;
+      }
+    }
+    const bool sound = all.m > -INFINITY && all.m < INFINITY && all.s == all.s;
+    const float log_s = sound ? log1pf(all.s) : NAN;
+    if (tid == 0) {
+      bool bad_target = false;
+      if (a.targets) {
+        const int t = __ldcg(a.targets + row);
+        bad_target = t >= a.vocab;
+        if (a.logprob) a.logprob[row] = t < 0 ? 0.f : bad_target ? NAN : (Logit<T>::one(x + t) - all.m) - log_s;
+      }
+      if (a.entropy) a.entropy[row] = sound ? log_s - all.w / (1.f + all.s) : NAN;
+      if (!sound || bad_target) atomicOr(a.status, (sound ? 0u : A3_DEV_NONFINITE_SCORE) | (bad_target ? A3_DEV_BAD_POSITION : 0u));
+    }
+    if (a.n_top > 0) {
+      const int n = a.n_top;
+      if (parts > 1) {  // the CTAs' lists, ranked by counting
+        const int total = parts * n;
+        for (int i = tid; i < total; i += LP_THREADS) s_cand[i] = cluster.map_shared_rank(s_top, i / n)[i % n];
+        __syncthreads();
+        if (tid < n) s_top[tid] = 0;  // read by this CTA alone
+        __syncthreads();
+        for (int i = tid; i < total; i += LP_THREADS) {
+          const unsigned long long k = s_cand[i];
+          int better = 0;
+          for (int j = 0; j < total; ++j) better += s_cand[j] > k;
+          if (k != 0 && better < n) s_top[better] = k;
+        }
+        __syncthreads();
+      }
+      if (warp == 0) {
+        // fewer elements above -inf than asked for: the lowest ids of those at -inf, then of NaNs
+        int have = __popc(__ballot_sync(0xffffffffu, lane < n && s_top[lane < n ? lane : 0] != 0));
+        for (int pass = 0; pass < 2 && have < n; ++pass) {
+          for (int i0 = 0; i0 < a.vocab && have < n; i0 += 32) {
+            const int i = i0 + lane;
+            const uint32_t o = i < a.vocab ? ordered(Logit<T>::one(x + i)) : 0xffffffffu;
+            const uint32_t these = __ballot_sync(0xffffffffu, o == (pass == 0 ? LP_NONE : 0u));
+            const int at = have + __popc(these & ((1u << lane) - 1));
+            if ((these >> lane & 1) && at < n) s_top[at] = lp_key(o, i);
+            have = min(n, have + __popc(these));
+            __syncwarp();
+          }
+        }
+        __syncwarp();
+        if (lane < n) {
+          const unsigned long long k = s_top[lane];
+          a.top_ids[(long long)row * n + lane] = key_id(k);
+          a.top_logprobs[(long long)row * n + lane] = sound ? (unordered((uint32_t)(k >> 32)) - all.m) - log_s : NAN;
+        }
+      }
+    }
+  }
+  if (parts > 1) cluster.sync();  // nobody leaves while its shared memory is read
+}
+
+template <typename T>
+static int logprobs_launch(const a3_handle* h, const LogprobArgs& a, cudaStream_t st) {
+  // CTAs per row: as many as the device holds at two per SM, and no fewer than 2 048 elements for each
+  int parts = 1;
+  while (parts < 8 && (long long)a.M * parts * 2 <= 2 * h->sm_count && a.vocab / (2 * parts) >= 2048) parts *= 2;
+  if ((long long)a.M * parts > 0x7fffffffll) return A3_EINVAL;
+  A3_CUDA(launch_pdl_cluster(parts, logprobs_kernel<T>, dim3((unsigned)(a.M * parts)), dim3(LP_THREADS), 0, st, a));
+  return launched();
+}
+
+}  // namespace a3
+
+using namespace a3;
+
+extern "C" int a3_token_logprobs(const a3_handle* h, const void* logits, int type, size_t row_stride, int M, int vocab,
+                                 const int32_t* targets, int n_top, float* logprob_out, float* entropy_out, int32_t* top_ids_out,
+                                 float* top_logprobs_out, a3_stream stream) {
+  if (!h || M < 0 || vocab <= 0 || n_top < 0 || n_top > vocab) return A3_EINVAL;
+  if (n_top > A3_LOGPROBS_MAX_TOP || type < A3_LOGITS_FP32 || type > A3_LOGITS_FP16) return A3_EUNSUPPORTED;
+  int device = -1;
+  if (cudaGetDevice(&device) != cudaSuccess || device != h->device) return A3_EINVAL;
+  if (M == 0) return A3_OK;
+  if (!targets != !logprob_out || !top_ids_out != (n_top == 0) || !top_logprobs_out != (n_top == 0)) return A3_EINVAL;
+  if (!logits || (uintptr_t)logits % (type == A3_LOGITS_FP32 ? 4 : 2)) return A3_EINVAL;
+  if ((M > 1 && row_stride < (size_t)vocab) || row_stride > (size_t)1 << 40) return A3_EINVAL;
+  const LogprobArgs a{logits, (long long)row_stride, M, vocab, targets, n_top, logprob_out, entropy_out, top_ids_out, top_logprobs_out, h->dev_status};
+  cudaStream_t st = (cudaStream_t)stream;
+  ProfScope prof(h, A3_K_FIRST_TOKEN, st);
+  return type == A3_LOGITS_FP32 ? logprobs_launch<float>(h, a, st) : type == A3_LOGITS_BF16 ? logprobs_launch<bf16>(h, a, st)
+                                                                                            : logprobs_launch<__half>(h, a, st);
+}

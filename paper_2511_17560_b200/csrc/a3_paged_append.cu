@@ -1,0 +1,167 @@
+// Rows into a paged cache (a3_paged_append): keys rotated to their positions, values as they are, queries rotated beside them.
+//
+// A row is cut into units of 16 elements of one head that rotate among themselves: for pairs (i, i + D/2) the two 16-byte vectors at
+// 8j and 8j + D/2, for pairs (2i, 2i+1) two neighbouring vectors.  One thread moves one unit: its two loads do not depend on
+// where the row goes, so they are on their way while the page is looked up.  Bound by HBM where rows are many and by
+// the chain slot -> page -> store where they are few.
+#include <cuda_fp8.h>
+
+#include "a3_internal.cuh"
+#include "a3_paged.cuh"
+
+namespace a3 {
+
+constexpr int PA_THREADS = 256;
+
+struct AppendArgs {
+  char *k_pages, *v_pages;
+  long long page_stride;  // bytes
+  int n_pages, page_size;
+  const float *k_scale, *v_scale;
+  const int32_t *table, *row_seq, *row_slot, *row_pos;
+  int n_seqs, max_pages;
+  const bf16 *q, *k, *v;
+  long long q_stride, k_stride, v_stride, q_out_stride;  // elements
+  bf16* q_out;
+  int M, q_heads, kv_heads;  // q_heads 0: no queries
+  const float2* tab;
+  int max_pos;
+  bool rotate;
+  uint32_t* status;
+};
+
+__device__ __forceinline__ uint2 pack8_e4m3(const float* f, float scale) {
+  uint32_t h[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {  // one rounding, from the rotated fp32 value; beyond the largest value: the largest value
+    float2 t = make_float2(__fdiv_rn(f[2 * i], scale), __fdiv_rn(f[2 * i + 1], scale));
+    h[i] = __nv_cvt_float2_to_fp8x2(t, __NV_SATFINITE, __NV_E4M3);
+  }
+  return make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
+}
+
+template <int D, int LAYOUT, bool F8>
+__global__ void __launch_bounds__(PA_THREADS)
+paged_append_kernel(const AppendArgs a) {
+  pdl_wait();
+  pdl_launch_dependents();
+  constexpr int UPH = D / 16;  // units per head
+  const int heads = a.q_heads + 2 * a.kv_heads;
+  const unsigned upr = (unsigned)heads * UPH;
+  const unsigned long long idx = (unsigned long long)blockIdx.x * PA_THREADS + threadIdx.x;
+  const long long r = (long long)(idx / upr);
+  if (r >= a.M) return;
+  const int u = (int)(idx % upr), j = u % UPH;
+  int head = u / UPH;
+  const int what = head < a.q_heads ? 0 : head < a.q_heads + a.kv_heads ? 1 : 2;  // q, k, v
+  if (what) head -= a.q_heads + (what == 2 ? a.kv_heads : 0);
+  const bf16* src = (what == 0 ? a.q + r * a.q_stride : what == 1 ? a.k + r * a.k_stride : a.v + r * a.v_stride) + head * D;
+  const bool halves = LAYOUT == 0 && what != 2;
+  const int lo = halves ? 8 * j : 16 * j, hi = halves ? lo + D / 2 : lo + 8;
+  const uint4 x0 = __ldcs(reinterpret_cast<const uint4*>(src + lo)), x1 = __ldcs(reinterpret_cast<const uint4*>(src + hi));
+
+  const int seq = __ldcg(a.row_seq + r), slot = __ldcg(a.row_slot + r);  // what a launch before this one may have written: past L1
+  if (seq < 0) return;  // padding
+  const int pos = a.row_pos ? __ldcg(a.row_pos + r) : slot;
+  const unsigned turn = pos < 0 ? 0u - (unsigned)pos : (unsigned)pos;
+  bool bad = seq >= a.n_seqs || slot < 0 || slot / a.page_size >= a.max_pages || (a.rotate && turn >= (unsigned)a.max_pos);
+  int page = 0;
+  if (!bad) {
+    page = __ldcg(a.table + (long long)seq * a.max_pages + slot / a.page_size);
+    bad = page < 0 || page >= a.n_pages;
+  }
+  if (bad) {
+    if (u == 0) atomicOr(a.status, A3_DEV_BAD_POSITION);
+    return;
+  }
+  float f[16];
+  unpack8(x0, f);
+  unpack8(x1, f + 8);
+  if (what != 2 && a.rotate) {
+    const float sgn = pos < 0 ? -1.f : 1.f;
+    const float4* tr = reinterpret_cast<const float4*>(a.tab + (size_t)turn * (D / 2) + 8 * j);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float4 t = __ldg(tr + e);  // (cos, sin) of frequencies 8j + 2e and 8j + 2e + 1
+      const int p = LAYOUT == 0 ? 2 * e : 4 * e, step = LAYOUT == 0 ? 1 : 2, mate = LAYOUT == 0 ? 8 : 1;
+      const float a0 = f[p], b0 = f[p + mate], a1 = f[p + step], b1 = f[p + step + mate], s0 = sgn * t.y, s1 = sgn * t.w;
+      f[p] = a0 * t.x - b0 * s0;
+      f[p + mate] = a0 * s0 + b0 * t.x;
+      f[p + step] = a1 * t.z - b1 * s1;
+      f[p + step + mate] = a1 * s1 + b1 * t.z;
+    }
+  }
+  if (what == 0) {
+    bf16* dst = a.q_out + r * a.q_out_stride + head * D;
+    *reinterpret_cast<uint4*>(dst + lo) = pack8(f);
+    *reinterpret_cast<uint4*>(dst + hi) = pack8(f + 8);
+    return;
+  }
+  char* dst = (what == 1 ? a.k_pages : a.v_pages) + page * a.page_stride + ((long long)(slot % a.page_size) * a.kv_heads + head) * (D * (F8 ? 1 : 2));
+  if (F8) {
+    const float scale = (what == 1 ? a.k_scale : a.v_scale)[head];
+    *reinterpret_cast<uint2*>(dst + lo) = pack8_e4m3(f, scale);
+    *reinterpret_cast<uint2*>(dst + hi) = pack8_e4m3(f + 8, scale);
+  } else {
+    *reinterpret_cast<uint4*>(dst + 2 * lo) = pack8(f);
+    *reinterpret_cast<uint4*>(dst + 2 * hi) = pack8(f + 8);
+  }
+}
+
+int paged_cache_check(const a3_handle* h, const a3_paged_cache* c) {
+  int device = -1;
+  if (cudaGetDevice(&device) != cudaSuccess || device != h->device) return A3_EINVAL;
+  if (!c->k_pages || !c->v_pages || c->n_pages <= 0 || c->page_size <= 0) return A3_EINVAL;
+  if (c->type != A3_CACHE_BF16 && c->type != A3_CACHE_E4M3) return A3_EUNSUPPORTED;
+  if (c->type == A3_CACHE_E4M3 && (!c->k_scale || !c->v_scale)) return A3_EINVAL;
+  if (((uintptr_t)c->k_pages | (uintptr_t)c->v_pages | c->page_stride) & 15) return A3_EINVAL;
+  const unsigned long long entry = (unsigned long long)h->m.n_kv_heads * h->m.head_dim * (c->type == A3_CACHE_BF16 ? 2 : 1);
+  if (c->page_stride < entry * c->page_size || c->page_stride > (1ull << 62) / (unsigned)c->n_pages) return A3_EINVAL;
+  return A3_OK;
+}
+
+}  // namespace a3
+
+using namespace a3;
+
+extern "C" int a3_paged_append(const a3_handle* h, const a3_paged_cache* cache, const int32_t* page_table, int n_seqs, int max_pages,
+                               const int32_t* row_seq, const int32_t* row_slot, const int32_t* row_pos, int rotate, const void* q_rows,
+                               size_t q_stride, const void* k_rows, size_t k_stride, const void* v_rows, size_t v_stride, int M, void* q_out,
+                               size_t q_out_stride, a3_stream stream) {
+  if (!h || !cache || M < 0 || n_seqs < 0 || max_pages < 0) return A3_EINVAL;
+  A3_TRY(paged_cache_check(h, cache));
+  if (M == 0) return A3_OK;
+  if (!page_table || !row_seq || !row_slot || !k_rows || !v_rows || !q_rows != !q_out) return A3_EINVAL;
+  if (((uintptr_t)q_rows | (uintptr_t)k_rows | (uintptr_t)v_rows | (uintptr_t)q_out) & 15) return A3_EINVAL;
+  const a3_model_desc& m = h->m;
+  const size_t qd = (size_t)m.n_q_heads * m.head_dim, kvd = (size_t)m.n_kv_heads * m.head_dim;
+  if (k_stride < kvd || v_stride < kvd || (q_rows && (q_stride < qd || q_out_stride < qd))) return A3_EINVAL;
+  if ((k_stride | v_stride | (q_rows ? q_stride | q_out_stride : 0)) % 8) return A3_EINVAL;
+  const size_t most = (size_t)1 << 40;  // elements between rows: offsets stay inside 63 bits
+  if (k_stride > most || v_stride > most || (q_rows && (q_stride > most || q_out_stride > most))) return A3_EINVAL;
+  AppendArgs a{};
+  a.k_pages = (char*)cache->k_pages, a.v_pages = (char*)cache->v_pages;
+  a.page_stride = (long long)cache->page_stride, a.n_pages = cache->n_pages, a.page_size = cache->page_size;
+  a.k_scale = cache->k_scale, a.v_scale = cache->v_scale;
+  a.table = page_table, a.row_seq = row_seq, a.row_slot = row_slot, a.row_pos = row_pos;
+  a.n_seqs = n_seqs, a.max_pages = max_pages;
+  a.q = (const bf16*)q_rows, a.k = (const bf16*)k_rows, a.v = (const bf16*)v_rows;
+  a.q_stride = (long long)q_stride, a.k_stride = (long long)k_stride, a.v_stride = (long long)v_stride, a.q_out_stride = (long long)q_out_stride;
+  a.q_out = (bf16*)q_out;
+  a.M = M, a.q_heads = q_rows ? m.n_q_heads : 0, a.kv_heads = m.n_kv_heads;
+  a.tab = h->rope_tab, a.max_pos = m.max_positions, a.rotate = rotate != 0, a.status = h->dev_status;
+  const unsigned long long units = (unsigned long long)M * (a.q_heads + 2 * a.kv_heads) * (m.head_dim / 16);
+  const unsigned long long blocks = (units + PA_THREADS - 1) / PA_THREADS;
+  if (blocks > 0x7fffffffull) return A3_EINVAL;
+  cudaStream_t st = (cudaStream_t)stream;
+  ProfScope prof(h, A3_K_ROWS, st);
+  auto go = [&](auto kernel) { return launch_pdl(kernel, dim3((unsigned)blocks), dim3(PA_THREADS), 0, st, a); };
+  const bool f8 = cache->type == A3_CACHE_E4M3;
+  auto layout = [&](auto d) {
+    constexpr int DD = decltype(d)::value;
+    return m.rope_layout == 0 ? (f8 ? go(paged_append_kernel<DD, 0, true>) : go(paged_append_kernel<DD, 0, false>))
+                              : (f8 ? go(paged_append_kernel<DD, 1, true>) : go(paged_append_kernel<DD, 1, false>));
+  };
+  A3_CUDA(m.head_dim == 64 ? layout(std::integral_constant<int, 64>{}) : layout(std::integral_constant<int, 128>{}));
+  return launched();
+}

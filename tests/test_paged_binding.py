@@ -1,0 +1,137 @@
+"""What the binding of the paged-cache calls and of the log probabilities refuses, and what it hands on.  The library calls
+themselves are replaced; nothing here needs a GPU."""
+import ctypes
+import os
+import subprocess
+from dataclasses import replace
+
+import pytest
+import torch
+
+from paper_2511_17560_b200 import a3
+from paper_2511_17560_b200 import workloads as W
+
+
+class Recorder:
+    def __init__(self, lib):
+        self._lib, self.calls = lib, []
+
+    def __getattr__(self, name):
+        return getattr(self._lib, name)
+
+    def a3_paged_attention_workspace_bytes(self, h):
+        return 512
+
+    def _note(self, *args):
+        self.calls.append(args)
+        return 0
+
+    a3_paged_append = a3_paged_attention = a3_token_logprobs = _note
+
+
+@pytest.fixture
+def eng(monkeypatch):
+    lib = Recorder(a3._load())
+    monkeypatch.setattr(a3, "_load", lambda: lib)
+    monkeypatch.setattr(a3, "_stream", lambda: 0)
+    e = a3.A3.__new__(a3.A3)
+    e.shape, e._h, e._ws, e.device = replace(W.TINY, n_q_heads=4, n_kv_heads=2), None, None, torch.device("cpu")
+    e.calls = lib.calls
+    return e
+
+
+def pages(dtype=torch.bfloat16, n=3, size=16, heads=2, d=64):
+    return torch.zeros((n, size, heads, d), dtype=torch.uint8 if dtype == torch.float8_e4m3fn else dtype).view(dtype)
+
+
+def i32(*x):
+    return torch.tensor(x, dtype=torch.int32)
+
+
+def refused(call, *args, **kw):
+    with pytest.raises(a3.A3Error) as e:
+        call(*args, **kw)
+    assert e.value.status == -1
+
+
+def test_cache_layouts():
+    k = pages()
+    c = a3.PagedCache(k, pages())
+    assert (c.desc.page_stride, c.desc.n_pages, c.desc.page_size, c.desc.type) == (16 * 2 * 64 * 2, 3, 16, 0)
+    both = torch.zeros((3, 2, 16, 2, 64), dtype=torch.bfloat16)
+    assert a3.PagedCache(both[:, 0], both[:, 1]).desc.page_stride == 2 * 16 * 2 * 64 * 2
+    s, f8 = torch.ones(2), torch.float8_e4m3fn
+    c = a3.PagedCache(pages(f8), pages(f8), s, s)
+    assert (c.desc.page_stride, c.desc.type) == (16 * 2 * 64, 1)
+    for args in [(k, pages(n=4)), (k, pages(torch.float16)), (pages(torch.float16),) * 2, (k, k, s, s), (pages(f8), pages(f8)), (pages(f8), pages(f8), s, None),
+                 (pages(f8), pages(f8), s, torch.ones(3)), (pages(f8), pages(f8), s, s.double()), (k[:, ::2], k[:, ::2]), (k[0], k[0]),
+                 (k.transpose(1, 2),) * 2, (k, both[:, 0]), (k[:0], k[:0])]:
+        refused(a3.PagedCache, *args)
+
+
+def test_append_arguments(eng):
+    cache, table = a3.PagedCache(pages(), pages()), torch.zeros((2, 2), dtype=torch.int32)
+    wide = torch.zeros((5, 8, 64), dtype=torch.bfloat16)
+    q, k, v, seq = wide[:, :4], wide[:, 4:6], wide[:, 6:], i32(0, 0, 1, 1, -1)
+    out = eng.paged_append(cache, table, seq, seq, k, v, q_rows=q)
+    args = eng.calls[-1]
+    assert out.shape == (5, 4, 64) and out.is_contiguous()
+    assert args[3:5] == (2, 2) and args[7:9] == (None, 1) and args[10] == 512 and args[12] == 512 and args[14:16] == (512, 5) and args[17] == 256
+    assert eng.paged_append(cache, table, seq, seq, k, v, rotate=False) is None and eng.calls[-1][8:11] == (0, None, 0)
+    calls = len(eng.calls)
+    flat = torch.zeros((5, 64, 2), dtype=torch.bfloat16).transpose(1, 2)
+    for kw in [dict(page_table=table.long()), dict(page_table=table[0]), dict(page_table=torch.zeros((2, 4), dtype=torch.int32)[:, ::2]), dict(row_seq=seq[:4]), dict(row_seq=seq.long()), dict(row_slot=seq[::2]),
+               dict(row_pos=seq[:2]), dict(row_pos=seq.float()), dict(k_rows=k.float()), dict(k_rows=k[:4]), dict(k_rows=flat), dict(v_rows=q),
+               dict(v_rows=v[..., :32]), dict(q_rows=k), dict(q_rows=None, q_out=out), dict(q_out=out.float()), dict(q_out=out[:4]),
+               dict(cache=a3.PagedCache(pages(heads=4), pages(heads=4))), dict(cache=a3.PagedCache(pages(d=128), pages(d=128)))]:
+        refused(eng.paged_append, **{**dict(cache=cache, page_table=table, row_seq=seq, row_slot=seq, k_rows=k, v_rows=v, q_rows=q), **kw})
+    assert len(eng.calls) == calls
+
+
+def test_attention_arguments(eng):
+    cache, table, lens = a3.PagedCache(pages(), pages()), torch.zeros((3, 2), dtype=torch.int32), i32(5, 0, 32)
+    q = torch.zeros((3, 6, 64), dtype=torch.bfloat16)[:, 1:5]
+    out, lse = eng.paged_attention(cache, table, lens, q, want_lse=True)
+    args = eng.calls[-1]
+    assert out.shape == (3, 4, 64) and lse.shape == (3, 4) and lse.dtype == torch.float32
+    assert args[3:5] == (3, 2) and args[7] == 384 and args[8] == 64 ** -0.5 and args[12] == 512
+    given = torch.empty((3, 4, 64), dtype=torch.bfloat16)
+    out, lse = eng.paged_attention(cache, table, lens, q, scale=0.5, out=given)
+    assert out is given and lse is None and eng.calls[-1][8] == 0.5 and eng.calls[-1][10] is None
+    calls = len(eng.calls)
+    for kw in [dict(cache_len=lens[:2]), dict(cache_len=lens.long()), dict(cache_len=lens[None]), dict(page_table=table.long()), dict(page_table=table[:2]),
+               dict(q_rows=q.float()), dict(q_rows=q[:2]), dict(q_rows=q[:, :2]), dict(q_rows=q[..., :32]), dict(out=given[:2]), dict(out=given.float()),
+               dict(cache=a3.PagedCache(pages(heads=1), pages(heads=1)))]:
+        refused(eng.paged_attention, **{**dict(cache=cache, page_table=table, cache_len=lens, q_rows=q), **kw})
+    assert len(eng.calls) == calls
+
+
+def test_logprob_arguments(eng):
+    x = torch.zeros((3, 80), dtype=torch.bfloat16)
+    logprob, entropy, ids, lps = eng.token_logprobs(x[:, 1:70], i32(0, 1, -1), 4)
+    assert logprob.shape == entropy.shape == (3,) and ids.shape == lps.shape == (3, 4) and ids.dtype == torch.int32
+    assert eng.calls[-1][2:6] == (1, 80, 3, 69) and eng.calls[-1][7] == 4
+    logprob, entropy, ids, lps = eng.token_logprobs(x)
+    assert logprob is ids is lps is None and eng.calls[-1][6:9] == (None, 0, None)
+    calls = len(eng.calls)
+    for args in [(x[0],), (x.double(),), (x.t(),), (x[:, ::2],), (x[:, :0],), (x, i32(0, 1)), (x, i32(0, 1, 2).long()), (x, i32(0, 1, 2)[None])]:
+        refused(eng.token_logprobs, *args)
+    assert len(eng.calls) == calls
+
+
+def test_cache_struct_matches_the_header(tmp_path):
+    lines = ['printf("%zu\\n", sizeof(a3_paged_cache));'] + [f'printf("%zu\\n", offsetof(a3_paged_cache, {f}));' for f, _ in a3.PagedCacheDesc._fields_]
+    src, exe = tmp_path / "layout.c", tmp_path / "layout"
+    src.write_text('#include <stdio.h>\n#include <stddef.h>\n#include "a3.h"\nint main(void) {\n' + "\n".join(lines) + "\nreturn 0; }\n")
+    inc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include")
+    subprocess.run(["gcc", "-std=c99", "-I", inc, str(src), "-o", str(exe)], check=True)
+    got = [int(s) for s in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split()]
+    assert got == [ctypes.sizeof(a3.PagedCacheDesc)] + [getattr(a3.PagedCacheDesc, f).offset for f, _ in a3.PagedCacheDesc._fields_]
+
+
+def test_null_handles():
+    lib = a3._load()
+    assert lib.a3_paged_attention_workspace_bytes(None) == 0
+    assert lib.a3_paged_append(None, None, None, 0, 0, None, None, None, 0, None, 0, None, 0, None, 0, 0, None, 0, None) == -1
+    assert lib.a3_paged_attention(None, None, None, 0, 0, None, None, 0, 1.0, None, None, None, 0, None) == -1
+    assert lib.a3_token_logprobs(None, None, 0, 0, 0, 1, None, 0, None, None, None, None, None) == -1
