@@ -26,9 +26,10 @@
 
 namespace a3 {
 
-constexpr int PD_WARPS = 4, PD_THREADS = 32 * PD_WARPS;
-constexpr int PD_STAGE = 8192;                 // bytes of a tile: keys in the lower half, values in the upper
-constexpr int PD_CTAS = 2;                     // per SM
+constexpr int PD_CTAS = 2;       // per SM
+constexpr int PD_WARPS = 4;       // of a CTA
+constexpr float LN2 = 0.693147180559945309f;
+constexpr float PD_SLACK = 8.f;  // see the running softmax
 
 struct PagedAttnArgs {
   const char *k_pages, *v_pages;
@@ -48,6 +49,7 @@ struct PagedAttnArgs {
   struct PartMeta* meta;  // [parts]
   float* part_o;          // [parts][units][2][unit][D]
   float2* part_ml;        // [parts][units][2][unit]
+  float* first_o;         // [parts][units][warps][unit][D]: see below
   uint32_t* status;
 };
 // The sequence that a part begins with: its number, its first tile on the line and its tiles; the tiles on the line, the parts that share them.
@@ -56,24 +58,51 @@ struct PartMeta {
   int seq, active;
 };
 
-__device__ __forceinline__ long long part_begin(long long p, long long total, long long active) { return p * total / active; }
-__device__ __forceinline__ long long part_of(long long tile, long long total, long long active) { return ((tile + 1) * active - 1) / total; }
+// The line cut into `active` parts, the first ones a tile longer where it does not divide: one division, of 32 bits as a rule (one of 64
+// takes 200 clocks).
+struct Parts {
+  long long size, more;  // tiles of a part; parts that have one more
+  __device__ Parts(long long total, int active) {
+    if (total <= 0xffffffffll) {
+      const unsigned q = (unsigned)total / (unsigned)active;
+      size = q, more = (unsigned)total - q * (unsigned)active;
+    } else {
+      size = total / active, more = total - size * active;
+    }
+  }
+  __device__ long long begin(int p) const { return p * size + (p < more ? p : more); }
+  __device__ int of(long long tile) const {
+    const long long longer = more * (size + 1);
+    if (tile < longer) return quotient(tile, size + 1);
+    return (int)more + quotient(tile - longer, size);
+  }
+  __device__ static int quotient(long long a, long long b) { return a <= 0xffffffffll && b <= 0xffffffffll ? (int)((unsigned)a / (unsigned)b) : (int)(a / b); }
+};
 
 __device__ __forceinline__ uint32_t movmatrix(uint32_t x) {
   uint32_t y;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-__device__ __forceinline__ void mma_f16(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+// D(16x8, fp32) += A(16x16, row) * B(16x8, col), fp16 or bf16; not volatile: the compiler may place it among the loads
+template <bool H>
+__device__ __forceinline__ void mma_any(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if constexpr (H)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t two) {
   uint32_t y;
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y) : "h"((unsigned short)two));
   return y;
+}
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;\n" ::"r"(dst), "l"(src));
 }
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -87,11 +116,12 @@ __device__ __forceinline__ uint32_t pack2h(float a, float b) {
 
 template <int D, bool F8, int NT>
 struct PagedCfg {
-  static constexpr int ROWB = D * (F8 ? 1 : 2), CH = ROWB / 16, KT = PD_STAGE / 2 / ROWB, HN = 8 * NT;
-  static constexpr int STAGES = D == 128 && NT == 2 ? 2 : 3;  // what leaves room for two CTAs per SM
-  static constexpr int SLOT = HN * D * 4;  // bytes of one partial output in shared memory
-  static constexpr int RING = STAGES * PD_STAGE, SMEM = PD_WARPS * (RING + SLOT);
-  static_assert(SLOT <= RING, "a warp's second partial output lies in its ring");
+  static constexpr int ROWB = D * (F8 ? 1 : 2), CH = ROWB / 16, HN = 8 * NT;
+  static constexpr int WARPS = PD_WARPS, THREADS = 32 * WARPS;
+  static constexpr int STAGE = 8192, HALF = STAGE / 2;  // bytes of a tile: keys in the lower half, values in the upper
+  static constexpr int KT = HALF / ROWB, STAGES = 3, RING = STAGES * STAGE;
+  static constexpr int SMEM = WARPS * RING;
+  static_assert(HN * D * 4 <= RING, "a warp's last partial output lies in its ring");
   __device__ static uint32_t at(int row, int chunk) {  // swizzled so that eight rows of one chunk column cover all banks
     return row * ROWB + ((CH == 4 ? chunk ^ ((row >> 1) & 3) : chunk ^ (row & 7)) << 4);
   }
@@ -103,26 +133,32 @@ struct SlotInfo {
   int seq;                 // -1: empty
 };
 
-template <int D, bool F8, int NT>
-__global__ void __launch_bounds__(PD_THREADS, PD_CTAS)
+// WHOLE: a tile never crosses a page (page_size is a multiple of KT), so that its rows lie at one distance from each other.
+template <int D, bool F8, int NT, bool WHOLE>
+__global__ void __launch_bounds__(PagedCfg<D, F8, NT>::THREADS, PD_CTAS)
 paged_attention_kernel(const PagedAttnArgs a) {
   using C = PagedCfg<D, F8, NT>;
-  constexpr int KT = C::KT, CH = C::CH, HN = C::HN, SUB = KT / 16, MT = D / 16;
+  constexpr int KT = C::KT, CH = C::CH, HN = C::HN, SUB = KT / 16, MT = D / 16, WARPS = C::WARPS;
   extern __shared__ __align__(1024) char smem[];
-  __shared__ long long s_scan[PD_WARPS], s_warp_first[PD_WARPS], s_warp_seqtile[PD_WARPS];
-  __shared__ int s_warp_seq[PD_WARPS];
-  __shared__ SlotInfo s_info[2 * PD_WARPS];
-  __shared__ float s_m[2 * PD_WARPS][HN], s_l[2 * PD_WARPS][HN];
+  __shared__ long long s_scan[WARPS], s_warp_first[WARPS];
+  __shared__ int s_warp_seq[WARPS], s_warp_len[WARPS];
+  constexpr int TILES = 8, PAGES = 4, KEYS = WHOLE ? 1 : KT;
+  __shared__ int4 s_tile[WARPS][TILES];  // of the tiles looked up, not yet computed: sequence, its length, tile in it, its first entry in its page
+  __shared__ int s_page[WARPS][PAGES][KEYS], s_ent[WARPS][PAGES][KEYS];  // page of a tile or, where it may cross pages, page and entry of each key
+  __shared__ SlotInfo s_info[2 * WARPS];
+  __shared__ float s_m[2 * WARPS][HN], s_l[2 * WARPS][HN];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int units = a.kv_heads * a.groups, hu = blockIdx.x % units, part = blockIdx.x / units;
   const int kvh = hu / a.groups, h0 = kvh * a.group + hu % a.groups * a.unit, hn = min(a.unit, (kvh + 1) * a.group - h0);
   char* ring = smem + warp * C::RING;
   const uint32_t ring_u = smem_u32(ring);
-  float* slot0 = reinterpret_cast<float*>(smem + PD_WARPS * C::RING + warp * C::SLOT);
-  if (threadIdx.x < 2 * PD_WARPS) s_info[threadIdx.x].seq = -1;
+  // A warp's first piece of a sequence, where it is partial and others follow it, waits in the workspace for the others' end.
+  float* first_o = a.first_o + (long long)blockIdx.x * WARPS * a.unit * D;
+  if (threadIdx.x < 2 * WARPS) s_info[threadIdx.x].seq = -1;
 
   pdl_wait();
   pdl_launch_dependents();
+  const float ks = F8 ? __ldcg(a.k_scale + kvh) : 1.f, vs = F8 ? __ldcg(a.v_scale + kvh) : 1.f;
 
   // ---- the line: every thread adds up the tiles of a stretch of sequences
   const long long cap = (long long)a.max_pages * a.page_size;
@@ -130,10 +166,12 @@ paged_attention_kernel(const PagedAttnArgs a) {
     const int n = __ldcg(a.lens + s);
     return n < 0 || n > cap ? 0 : n;
   };
-  const int per = (a.n_seqs + PD_THREADS - 1) / PD_THREADS, s0 = min(a.n_seqs, (int)threadIdx.x * per), s1 = min(a.n_seqs, s0 + per);
+  const int per = (a.n_seqs + C::THREADS - 1) / C::THREADS, s0 = min(a.n_seqs, (int)threadIdx.x * per), s1 = min(a.n_seqs, s0 + per);
   long long mine = 0;
+  int n0 = 0;  // the first of them
   for (int s = s0; s < s1; ++s) {
     const int n = length(s);
+    if (s == s0) n0 = n;
     mine += (n + KT - 1) / KT;
     if (n == 0 && part == 0) {  // nothing to attend to: no weight anywhere
       if (__ldcg(a.lens + s) != 0 && hu == 0) atomicOr(a.status, A3_DEV_BAD_POSITION);
@@ -154,24 +192,25 @@ paged_attention_kernel(const PagedAttnArgs a) {
   __syncthreads();
   long long total = 0, before = upto - mine;
 #pragma unroll
-  for (int w = 0; w < PD_WARPS; ++w) {
+  for (int w = 0; w < WARPS; ++w) {
     if (w < warp) before += s_scan[w];
     total += s_scan[w];
   }
-  const long long wanted = (total + PD_WARPS - 1) / PD_WARPS;  // a tile for each warp at least
+  const long long wanted = (total + WARPS - 1) / WARPS;  // a tile for each warp at least
   const int active = (int)(wanted < a.parts ? wanted : a.parts);
   if (total == 0 && blockIdx.x == 0 && threadIdx.x == 0) a.meta[0].active = 0;
   if (part >= active) return;
-  const long long c0 = part_begin(part, total, active), c1 = part_begin(part + 1, total, active);
-  auto warp_begin = [&](int w) { return c0 + (c1 - c0) * w / PD_WARPS; };
+  const Parts parts(total, active);
+  const long long c0 = parts.begin(part), c1 = parts.begin(part + 1);
+  auto warp_begin = [&](int w) { return c0 + (c1 - c0) * w / WARPS; };
   if (mine > 0) {
     for (int s = s0; s < s1; ++s) {
-      const long long n = (length(s) + KT - 1) / KT;
-      for (int w = 0; w < PD_WARPS; ++w) {
+      const int n = s == s0 ? n0 : length(s), tiles = (n + KT - 1) / KT;
+      for (int w = 0; w < WARPS; ++w) {
         const long long b = warp_begin(w);
-        if (b >= before && b < before + n) s_warp_seq[w] = s, s_warp_first[w] = before;
+        if (b >= before && b < before + tiles) s_warp_seq[w] = s, s_warp_first[w] = before, s_warp_len[w] = n;
       }
-      before += n;
+      before += tiles;
     }
   }
   __syncthreads();
@@ -179,96 +218,137 @@ paged_attention_kernel(const PagedAttnArgs a) {
   // ---- this warp's stretch
   const long long w0 = warp_begin(warp), w1 = warp_begin(warp + 1);
   const int count = (int)(w1 - w0);
-  if (hu == 0 && threadIdx.x == 0) {
-    const int s = s_warp_seq[0];
-    a.meta[part] = PartMeta{s_warp_first[0], (length(s) + KT - 1) / KT, total, s, active};
-  }
+  if (hu == 0 && threadIdx.x == 0)
+    a.meta[part] = PartMeta{s_warp_first[0], (s_warp_len[0] + KT - 1) / KT, total, s_warp_seq[0], active};
   if (count > 0) {
-    const long long kv_off = (long long)kvh * C::ROWB, entry = (long long)a.kv_heads * C::ROWB;
-    // where the copies are: sequence, its length, tile in it
-    int ls = s_warp_seq[warp], ln = length(ls), lt = (int)(w0 - s_warp_first[warp]);
-    // and the computation
-    int cs = ls, cn = ln, ct = lt;
-    long long cfirst = s_warp_first[warp];
-    constexpr int KPL = (KT + 31) / 32;
-    int page[KPL], ent[KPL];
-    auto look_up = [&] {  // the pages of the next tile, one lane for each key
+    const long long entry = (long long)a.kv_heads * C::ROWB;
+    const char *k_base = a.k_pages + (long long)kvh * C::ROWB + lane % CH * 16, *v_base = a.v_pages + (long long)kvh * C::ROWB + lane % CH * 16;
+    const long long step = 32 / CH * entry;
+    constexpr int RPI = 32 / CH;            // rows that a warp copies with one instruction
+    long long cfirst = s_warp_first[warp];  // first tile of the sequence that is computed
+
+    // Queries of a sequence, one head in eight for each group of four lanes, raw.  Those of the next one are fetched while a sequence is
+    // computed (where the registers suffice), the first ones before any key: behind the copies under way a load takes 2 us.
+    uint32_t qf[MT][NT][2], qn[MT][NT][2];
+    uint32_t(&qr)[MT][NT][2] = NT == 1 ? qn : qf;
+    int q_seq = s_warp_seq[warp];
+    auto load_q = [&] {
+      const bf16* q = a.q + q_seq * a.q_stride;
 #pragma unroll
-      for (int i = 0; i < KPL; ++i) {
-        const int key = lt * KT + 32 * i + lane;
-        const bool there = 32 * i + lane < KT && key < ln;
-        page[i] = -1, ent[i] = -1;
-        if (there) {
-          const int p = key / a.page_size;
-          ent[i] = key - p * a.page_size;
-          page[i] = __ldcg(a.table + (long long)ls * a.max_pages + p);
-        }
-      }
-    };
-    auto next_tile = [&](int& s, int& n, int& t) {
-      if (++t * KT >= n) {
-        t = 0;
-        do n = length(++s);
-        while (n == 0);
-      }
-    };
-    auto issue = [&](int stage) {
-      const uint32_t dst = ring_u + stage * PD_STAGE;
-      long long off[KPL];
+      for (int nt = 0; nt < NT; ++nt) {
+        const int h = nt * 8 + lane / 4;
+        const uint32_t* row = reinterpret_cast<const uint32_t*>(q + (h0 + h) * D);
 #pragma unroll
-      for (int i = 0; i < KPL; ++i) {
-        off[i] = -1;
-        if (ent[i] >= 0) {
-          if (page[i] >= 0 && page[i] < a.n_pages) off[i] = page[i] * a.page_stride + ent[i] * entry + kv_off;
-          else atomicOr(a.status, A3_DEV_BAD_POSITION);
-        }
-      }
-      constexpr int RPI = 32 / CH;  // rows a warp copies with one instruction
+        for (int ks = 0; ks < MT; ++ks)
 #pragma unroll
-      for (int i = 0; i < KT / RPI; ++i) {
-        const int r = i * RPI + lane / CH, c = lane % CH;
-        const long long o = __shfl_sync(0xffffffffu, off[i * RPI / 32], r & 31);
-        const bool there = o >= 0;  // rows that are not there are filled with zeros: nothing behind a sequence is read
-        const long long src = there ? o + c * 16 : 0;
-        cp_async16(dst + C::at(r, c), a.k_pages + src, there);
-        cp_async16(dst + PD_STAGE / 2 + C::at(r, c), a.v_pages + src, there);
+          for (int e = 0; e < 2; ++e) qr[ks][nt][e] = h < hn ? __ldcg(row + 8 * ks + (F8 ? 2 * (lane % 4) + e : lane % 4 + 4 * e)) : 0u;
       }
     };
 
-    uint32_t qf[MT][NT][2];
-    float o[MT][NT][4], m[NT][2], l[NT][2], cq[NT][2];
-    int left_ld = count;
-    look_up();
-    auto advance = [&](int stage) {  // one more tile under way
-      if (left_ld > 0) {
-        issue(stage);
-        if (--left_ld > 0) {
-          next_tile(ls, ln, lt);
-          look_up();
+    // Three steps of a tile, each in its own turn: its pages are looked up, three turns later its rows are copied, two turns after that it
+    // is computed.  Pages and rows come by asynchronous copies, so that no turn waits for an access that it makes itself.
+    int xs = q_seq, xn = s_warp_len[warp], xt = (int)(w0 - s_warp_first[warp]), xp = xt * KT / a.page_size, xe = xt * KT - xp * a.page_size;
+    int x_left = count, x_next = xs + 1 < a.n_seqs ? length(xs + 1) : 0;
+    auto look_up = [&](int j) {
+      if (x_left <= 0) return;
+      const int32_t* row = a.table + (long long)xs * a.max_pages;
+      if (lane == 0) s_tile[warp][j % TILES] = make_int4(xs, xn, xt, xe);
+      if constexpr (WHOLE) {
+        if (lane == 0) cp_async4(smem_u32(&s_page[warp][j % PAGES][0]), row + xp);
+      } else {
+#pragma unroll
+        for (int i = lane; i < KT; i += 32) {
+          const int key = xt * KT + i, p = key / a.page_size;
+          if (key < xn) cp_async4(smem_u32(&s_page[warp][j % PAGES][i]), row + p);
+          s_ent[warp][j % PAGES][i] = key < xn ? key - p * a.page_size : -1;
         }
       }
+      if (--x_left == 0) return;
+      if (++xt * KT >= xn) {
+        xt = xp = xe = 0;
+        ++xs;
+        xn = x_next;
+        while (xn == 0) xn = length(++xs);
+        x_next = xs + 1 < a.n_seqs ? length(xs + 1) : 0;
+      } else if (WHOLE && (xe += KT) == a.page_size) {
+        xe = 0;
+        ++xp;
+      }
+    };
+    auto copy = [&](int j) {  // rows that are not there are filled with zeros: nothing behind a sequence is read
+      if (j >= count) return;
+      const uint32_t dst = ring_u + j % C::STAGES * C::STAGE;
+      const int r0 = lane / CH;
+      if constexpr (WHOLE) {
+        const int4 x = s_tile[warp][j % TILES];
+        const int page = s_page[warp][j % PAGES][0];
+        const bool good = (unsigned)page < (unsigned)a.n_pages;
+        if (!good) atomicOr(a.status, A3_DEV_BAD_POSITION);
+        const int left = good ? x.y - x.z * KT : 0;
+        long long at = (good ? page * a.page_stride : 0) + (x.w + r0) * entry;
+        if (left >= KT) {
+#pragma unroll
+          for (int i = 0; i < KT / RPI; ++i, at += step) {
+            cp_async16(dst + C::at(r0 + i * RPI, lane % CH), k_base + at, true);
+            cp_async16(dst + C::HALF + C::at(r0 + i * RPI, lane % CH), v_base + at, true);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < KT / RPI; ++i, at += step) {
+            const bool there = r0 + i * RPI < left;
+            cp_async16(dst + C::at(r0 + i * RPI, lane % CH), k_base + (there ? at : 0), there);
+            cp_async16(dst + C::HALF + C::at(r0 + i * RPI, lane % CH), v_base + (there ? at : 0), there);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < KT / RPI; ++i) {
+          const int page = s_page[warp][j % PAGES][r0 + i * RPI], ent = s_ent[warp][j % PAGES][r0 + i * RPI];
+          const bool good = (unsigned)page < (unsigned)a.n_pages, there = ent >= 0 && good;
+          if (ent >= 0 && !good) atomicOr(a.status, A3_DEV_BAD_POSITION);
+          const long long at = there ? page * a.page_stride + ent * entry : 0;
+          cp_async16(dst + C::at(r0 + i * RPI, lane % CH), k_base + at, there);
+          cp_async16(dst + C::HALF + C::at(r0 + i * RPI, lane % CH), v_base + at, there);
+        }
+      }
+    };
+
+    float o[MT][NT][4], m[NT][2], l[NT][2], cq[NT][2];
+    load_q();
+#pragma unroll
+    for (int j = 0; j < 3; ++j) look_up(j);
+    cp_async_commit();
+    cp_async_wait<0>();
+    __syncwarp();
+    auto turn = [&](int j) {
+      copy(j);
+      look_up(j + 3);
       cp_async_commit();
     };
-#pragma unroll
-    for (int i = 0; i < C::STAGES - 1; ++i) advance(i);
+    static_assert(C::STAGES == 3, "two turns between the copy and its use, three between look-up and copy");
+    turn(0);
+    __syncwarp();  // a look-up may take the place of the page that another lane has just read
+    turn(1);
+    __syncwarp();
     bool fresh = true;
-    int piece0 = ct, n_pieces = 0;
+    int piece0 = 0;
     for (int i = 0; i < count; ++i) {
-      advance((i + C::STAGES - 1) % C::STAGES);
-      if (fresh) {  // queries of the sequence
+      turn(i + 2);
+      const int4 tile = s_tile[warp][i % TILES];
+      const int cs = tile.x, cn = tile.y, ct = tile.z;
+      if (fresh) {  // a sequence, or what is left of one, begins
         fresh = false;
         piece0 = ct;
-        const bf16* q = a.q + cs * a.q_stride;
+        if (q_seq != cs) {
+          q_seq = cs;
+          load_q();
+        }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          const int h = nt * 8 + lane / 4;
-          const uint32_t* row = reinterpret_cast<const uint32_t*>(q + (h0 + h) * D);
 #pragma unroll
-          for (int ks = 0; ks < MT; ++ks) {
+          for (int ks = 0; ks < MT; ++ks)
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
-              qf[ks][nt][e] = h < hn ? __ldcg(row + 8 * ks + (F8 ? 2 * (lane % 4) + e : lane % 4 + 4 * e)) : 0u;
-          }
+            for (int e = 0; e < 2; ++e) qf[ks][nt][e] = qr[ks][nt][e];
           float up = a.scale_log2;
           if (F8) {
             float most = 0.f;
@@ -285,7 +365,7 @@ paged_attention_kernel(const PagedAttnArgs a) {
             int ex = most > 0.f && most < INFINITY ? ilogbf(most) - 14 : 0;
             ex = max(-120, min(120, ex));
             const float down = __int_as_float((127 - ex) << 23);
-            up *= __int_as_float((127 + ex) << 23) * a.k_scale[kvh];
+            up *= __int_as_float((127 + ex) << 23) * ks;
 #pragma unroll
             for (int ks = 0; ks < MT; ++ks)
 #pragma unroll
@@ -306,75 +386,93 @@ paged_attention_kernel(const PagedAttnArgs a) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[mt][nt][e] = 0.f;
         }
+        if (NT == 1 && count - i > (cn + KT - 1) / KT - ct) {  // more sequences follow: of the next one, unless it is empty
+          ++q_seq;
+          load_q();
+        }
       }
       cp_async_wait<C::STAGES - 1>();
       __syncwarp();
-      const uint32_t kt_u = ring_u + i % C::STAGES * PD_STAGE, vt_u = kt_u + PD_STAGE / 2;
+      const uint32_t kt_u = ring_u + i % C::STAGES * C::STAGE, vt_u = kt_u + C::HALF;
 
-      // ---- S^T = K Q^T
+      // ---- S^T = K Q^T; all loads of 16 keys first, two sums of each product (a chain of eight would take 8 x 22 clocks)
       float s[SUB][NT][4];
+      constexpr int KL = F8 ? MT / 2 : MT;  // ldmatrix instructions for 16 rows
 #pragma unroll
       for (int sub = 0; sub < SUB; ++sub) {
+        uint32_t k[KL][4];
+        const int row = sub * 16 + (lane >> 3 & 1) * 8 + (lane & 7);
+#pragma unroll
+        for (int j = 0; j < KL; ++j) ldmatrix_x4(kt_u + C::at(row, 2 * j + (lane >> 4)), k[j][0], k[j][1], k[j][2], k[j][3]);
+        float odd[NT][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[sub][nt][e] = 0.f;
-        const int row = sub * 16 + (lane >> 3 & 1) * 8 + (lane & 7);
-        if constexpr (!F8) {
+          for (int e = 0; e < 4; ++e) s[sub][nt][e] = odd[nt][e] = 0.f;
 #pragma unroll
-          for (int ks = 0; ks < MT; ++ks) {
-            uint32_t k[4];
-            ldmatrix_x4(kt_u + C::at(row, 2 * ks + (lane >> 4)), k[0], k[1], k[2], k[3]);
+        for (int j = 0; j < KL; ++j) {
+          if constexpr (!F8) {
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma_bf16(s[sub][nt], k, qf[ks][nt][0], qf[ks][nt][1]);
-          }
-        } else {
-#pragma unroll
-          for (int ks = 0; ks < MT; ks += 2) {
-            uint32_t r[4];
-            ldmatrix_x4(kt_u + C::at(row, ks + (lane >> 4)), r[0], r[1], r[2], r[3]);
+            for (int nt = 0; nt < NT; ++nt)
+              mma_any<false>(j & 1 ? odd[nt] : s[sub][nt], k[j][0], k[j][1], k[j][2], k[j][3], qf[j][nt][0], qf[j][nt][1]);
+          } else {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const uint32_t k[4] = {e4m3x2_to_f16x2(r[2 * e]), e4m3x2_to_f16x2(r[2 * e + 1]), e4m3x2_to_f16x2(r[2 * e] >> 16),
-                                     e4m3x2_to_f16x2(r[2 * e + 1] >> 16)};
+              const uint32_t x = k[j][2 * e], y = k[j][2 * e + 1];
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) mma_f16(s[sub][nt], k, qf[ks + e][nt][0], qf[ks + e][nt][1]);
+              for (int nt = 0; nt < NT; ++nt)
+                mma_any<true>(e ? odd[nt] : s[sub][nt], e4m3x2_to_f16x2(x), e4m3x2_to_f16x2(y), e4m3x2_to_f16x2(x >> 16), e4m3x2_to_f16x2(y >> 16),
+                              qf[2 * j + e][nt][0], qf[2 * j + e][nt][1]);
             }
           }
         }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[sub][nt][e] += odd[nt][e];
       }
+      // values of the first 16 keys, on their way while the weights are formed
+      uint32_t v[KL][4];
+      auto load_v = [&](int sub) {
+        const int row = sub * 16 + (F8 ? lane >> 3 & 1 : lane >> 4) * 8 + (lane & 7);
+#pragma unroll
+        for (int j = 0; j < KL; ++j) ldmatrix_x4_trans(vt_u + C::at(row, 2 * j + (F8 ? lane >> 4 : lane >> 3 & 1)), v[j][0], v[j][1], v[j][2], v[j][3]);
+      };
+      load_v(0);
 
-      // ---- running softmax
+      // ---- running softmax: the reference m need not be the maximum, it only has to be near it.  It is raised, over the lanes that
+      // share a head and with everything rescaled, when a logit is more than 2^8 above it; weights are 256 at most.
       const int left = cn - ct * KT;  // keys from here on
-      float top[NT][2];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        top[nt][0] = top[nt][1] = -INFINITY;
-#pragma unroll
-        for (int sub = 0; sub < SUB; ++sub)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float t = s[sub][nt][e] * cq[nt][e & 1];
-            if (left < KT && sub * 16 + (e >> 1) * 8 + lane / 4 >= left) t = -INFINITY;
-            s[sub][nt][e] = t;
-            top[nt][e & 1] = fmaxf(top[nt][e & 1], t);
-          }
-      }
       bool grew = false;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
+        for (int sub = 0; sub < SUB; ++sub)
 #pragma unroll
-          for (int x = 4; x < 32; x <<= 1) top[nt][e] = fmaxf(top[nt][e], __shfl_xor_sync(0xffffffffu, top[nt][e], x));
-          grew |= top[nt][e] > m[nt][e];
-        }
+          for (int e = 0; e < 4; ++e) {
+            const float t = s[sub][nt][e] * cq[nt][e & 1];
+            s[sub][nt][e] = t;
+            grew |= t > m[nt][e & 1] + PD_SLACK;
+          }
+      if (left < KT) {  // the sequence ends in this tile; what `grew` made of the rows behind it only raises the reference needlessly
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int sub = 0; sub < SUB; ++sub)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (sub * 16 + (e >> 1) * 8 + lane / 4 >= left) s[sub][nt][e] = -INFINITY;
+      }
       if (__any_sync(0xffffffffu, grew)) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float now = fmaxf(m[nt][e], top[nt][e]);
+            float now = m[nt][e];
+#pragma unroll
+            for (int sub = 0; sub < SUB; ++sub) now = fmaxf(now, fmaxf(s[sub][nt][e], s[sub][nt][e + 2]));
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, x));
             const float f = now == -INFINITY ? 1.f : ex2(m[nt][e] - now);
             m[nt][e] = now;
             l[nt][e] *= f;
@@ -408,34 +506,26 @@ paged_attention_kernel(const PagedAttnArgs a) {
       // ---- O^T += V^T P^T
 #pragma unroll
       for (int sub = 0; sub < SUB; ++sub) {
-        if constexpr (!F8) {
-          const int row = sub * 16 + (lane >> 4) * 8 + (lane & 7);
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt) {
-            uint32_t v[4];
-            ldmatrix_x4_trans(vt_u + C::at(row, 2 * mt + (lane >> 3 & 1)), v[0], v[1], v[2], v[3]);
+        for (int j = 0; j < KL; ++j) {
+          if constexpr (!F8) {
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              mma_bf16(o[mt][nt], v, hi[sub][nt][0], hi[sub][nt][1]);
-              mma_bf16(o[mt][nt], v, lo[sub][nt][0], lo[sub][nt][1]);
-            }
-          }
-        } else {
-          const int row = sub * 16 + (lane >> 3 & 1) * 8 + (lane & 7);
+            for (int nt = 0; nt < NT; ++nt) mma_any<false>(o[j][nt], v[j][0], v[j][1], v[j][2], v[j][3], hi[sub][nt][0], hi[sub][nt][1]);
 #pragma unroll
-          for (int mt = 0; mt < MT; mt += 2) {
-            uint32_t r[4];
-            ldmatrix_x4_trans(vt_u + C::at(row, mt + (lane >> 4)), r[0], r[1], r[2], r[3]);
+            for (int nt = 0; nt < NT; ++nt) mma_any<false>(o[j][nt], v[j][0], v[j][1], v[j][2], v[j][3], lo[sub][nt][0], lo[sub][nt][1]);
+          } else {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               // a register holds dimensions (2i, 2i+1) of one key, then of the next: rows i and i + 8 of the product are those two
-              const uint32_t x = __byte_perm(r[2 * e], 0, 0x3120), y = __byte_perm(r[2 * e + 1], 0, 0x3120);
-              const uint32_t v[4] = {e4m3x2_to_f16x2(x), e4m3x2_to_f16x2(x >> 16), e4m3x2_to_f16x2(y), e4m3x2_to_f16x2(y >> 16)};
+              const uint32_t x = __byte_perm(v[j][2 * e], 0, 0x3120), y = __byte_perm(v[j][2 * e + 1], 0, 0x3120);
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) mma_f16(o[mt + e][nt], v, hi[sub][nt][0], hi[sub][nt][1]);
+              for (int nt = 0; nt < NT; ++nt)
+                mma_any<true>(o[2 * j + e][nt], e4m3x2_to_f16x2(x), e4m3x2_to_f16x2(x >> 16), e4m3x2_to_f16x2(y), e4m3x2_to_f16x2(y >> 16), hi[sub][nt][0],
+                              hi[sub][nt][1]);
             }
           }
         }
+        if (sub + 1 < SUB) load_v(sub + 1);
       }
       __syncwarp();
 
@@ -448,7 +538,6 @@ paged_attention_kernel(const PagedAttnArgs a) {
           for (int e = 0; e < 2; ++e)
 #pragma unroll
             for (int x = 4; x < 32; x <<= 1) l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], x);
-        const float vs = F8 ? a.v_scale[kvh] : 1.f;
         if (piece0 == 0 && ct == tiles - 1) {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
@@ -464,17 +553,18 @@ paged_attention_kernel(const PagedAttnArgs a) {
                   a.out[at * D + d] = __float2bfloat16(o[mt][nt][e] * f);
                   a.out[at * D + d + (F8 ? 1 : 8)] = __float2bfloat16(o[mt][nt][e + 2] * f);
                 }
-                if (a.lse && lane / 4 == 0) a.lse[at] = l[nt][e] == 0.f ? -INFINITY : (m[nt][e] + log2f(l[nt][e])) * 0.693147180559945309f;
+                if (a.lse && lane / 4 == 0) a.lse[at] = l[nt][e] == 0.f ? -INFINITY : (m[nt][e] + log2f(l[nt][e])) * LN2;
               }
             }
         } else {
-          const int which = n_pieces == 0 ? 0 : 1, info = 2 * warp + which;
-          float* dst = which == 0 ? slot0 : reinterpret_cast<float*>(ring);
+          const int which = i == count - 1, info = 2 * warp + which;  // partial and not the last: the first
+          float* dst = which == 0 ? first_o + warp * a.unit * D : reinterpret_cast<float*>(ring);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               const int h = nt * 8 + 2 * (lane % 4) + e;
+              if (which == 0 && h >= hn) continue;
 #pragma unroll
               for (int mt = 0; mt < MT; ++mt) {
                 const int d = mt * 16 + (F8 ? 2 * (lane / 4) : lane / 4);
@@ -485,17 +575,15 @@ paged_attention_kernel(const PagedAttnArgs a) {
             }
           if (lane == 0) s_info[info] = SlotInfo{cfirst, tiles, cs};
         }
-        ++n_pieces;
         fresh = true;
         if (ct == tiles - 1) cfirst += tiles;
       }
-      if (i + 1 < count) next_tile(cs, cn, ct);
     }
   }
   __syncthreads();
 
   // ---- what the warps hold of one sequence, merged
-  for (int i0 = 0; i0 < 2 * PD_WARPS; ++i0) {
+  for (int i0 = 0; i0 < 2 * WARPS; ++i0) {
     const SlotInfo info = s_info[i0];
     if (info.seq < 0) continue;
     bool first_of = true;
@@ -503,28 +591,34 @@ paged_attention_kernel(const PagedAttnArgs a) {
     if (!first_of) continue;
     const bool began = info.first < c0, goes_on = info.first + info.tiles > c1;
     const long long slot = ((long long)part * units + hu) * 2 + (began ? 0 : 1);
-    for (int x = threadIdx.x; x < hn * (D / 2); x += PD_THREADS) {
-      const int h = x / (D / 2), d = x % (D / 2) * 2;
-      float mm = -INFINITY;
-      for (int i = i0; i < 2 * PD_WARPS; ++i)
-        if (s_info[i].seq == info.seq) mm = fmaxf(mm, s_m[i][h]);
+    unsigned members = 0;
+#pragma unroll
+    for (int i = 0; i < 2 * WARPS; ++i) members |= (s_info[i].seq == info.seq) << i;
+    for (int x = threadIdx.x; x < hn * (D / 4); x += C::THREADS) {
+      const int h = x / (D / 4), d = x % (D / 4) * 4;
+      float f[2 * WARPS], mm = -INFINITY, ll = 0.f;
+#pragma unroll
+      for (int i = 0; i < 2 * WARPS; ++i) {
+        f[i] = members >> i & 1 ? s_m[i][h] : -INFINITY;
+        mm = fmaxf(mm, f[i]);
+      }
       const float ref = mm == -INFINITY ? 0.f : mm;
-      float ll = 0.f, ox = 0.f, oy = 0.f;
-      for (int i = i0; i < 2 * PD_WARPS; ++i)
-        if (s_info[i].seq == info.seq) {
-          const float f = ex2(s_m[i][h] - ref);
-          const float* src = reinterpret_cast<const float*>(i & 1 ? smem + i / 2 * C::RING : smem + PD_WARPS * C::RING + i / 2 * C::SLOT) + C::out_at(h, d);
-          ll += f * s_l[i][h];
-          ox += f * src[0];
-          oy += f * src[1];
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < 2 * WARPS; ++i)
+        if (members >> i & 1) {
+          const float g = ex2(f[i] - ref);
+          const float4 v = *reinterpret_cast<const float4*>((i & 1 ? reinterpret_cast<const float*>(smem + i / 2 * C::RING) : first_o + i / 2 * a.unit * D) + C::out_at(h, d));
+          ll += g * s_l[i][h];
+          o.x += g * v.x, o.y += g * v.y, o.z += g * v.z, o.w += g * v.w;
         }
       if (!began && !goes_on) {
-        const float f = ll == 0.f ? 0.f : 1.f / ll;
+        const float g = ll == 0.f ? 0.f : 1.f / ll;
         const long long at = (long long)info.seq * a.q_heads + h0 + h;
-        *reinterpret_cast<uint32_t*>(a.out + at * D + d) = pack2(ox * f, oy * f);
-        if (a.lse && d == 0) a.lse[at] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * 0.693147180559945309f;
+        *reinterpret_cast<uint2*>(a.out + at * D + d) = make_uint2(pack2(o.x * g, o.y * g), pack2(o.z * g, o.w * g));
+        if (a.lse && d == 0) a.lse[at] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * LN2;
       } else {
-        *reinterpret_cast<float2*>(a.part_o + (slot * a.unit + h) * D + d) = make_float2(ox, oy);
+        *reinterpret_cast<float4*>(a.part_o + (slot * a.unit + h) * D + d) = o;
         if (d == 0) a.part_ml[slot * a.unit + h] = make_float2(mm, ll);
       }
     }
@@ -532,42 +626,87 @@ paged_attention_kernel(const PagedAttnArgs a) {
 }
 
 // Block (p, unit, head): the sequence that part p begins with, if it began in the part before, from all parts that hold some of it.
+// A warp's lanes cover the head dimension; the warps take parts in turn.
+constexpr int PJ_WARPS = 4;
 template <int D>
-__global__ void __launch_bounds__(D / 2)
+__global__ void __launch_bounds__(32 * PJ_WARPS)
 paged_join_kernel(const PagedAttnArgs a) {
+  constexpr int V = D / 32;
+  extern __shared__ float s_f[];  // [parts] weights
+  __shared__ float s_red[2][PJ_WARPS], s_o[PJ_WARPS][D];
   pdl_wait();
   pdl_launch_dependents();
-  const int p = blockIdx.x + 1, hu = blockIdx.y, g = blockIdx.z, units = a.kv_heads * a.groups;
+  const int p = blockIdx.x + 1, hu = blockIdx.y, g = blockIdx.z, units = a.kv_heads * a.groups, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int kvh = hu / a.groups, h0 = kvh * a.group + hu % a.groups * a.unit, hn = min(a.unit, (kvh + 1) * a.group - h0);
   if (g >= hn) return;
-  const int active = __ldcg(&a.meta[0].active);
-  if (p >= active) return;
+  // all at once; what part p says is right only where there is such a part
+  const int active = __ldcg(&a.meta[0].active), seq = __ldcg(&a.meta[p].seq);
   const long long total = __ldcg(&a.meta[p].total), first = __ldcg(&a.meta[p].first), tiles = __ldcg(&a.meta[p].tiles);
-  if (first >= part_begin(p, total, active)) return;
-  const int from = (int)part_of(first, total, active), to = (int)part_of(first + tiles - 1, total, active);
+  if (p >= active) return;
+  const Parts parts(total, active);
+  if (first >= parts.begin(p)) return;
+  const int from = parts.of(first), n = parts.of(first + tiles - 1) - from + 1;
   if (from != p - 1) return;
-  const int d = threadIdx.x * 2;
-  float mm = -INFINITY, ll = 0.f, ox = 0.f, oy = 0.f;
-  for (int i = from; i <= to; ++i) {
-    const long long slot = ((long long)i * units + hu) * 2 + (i == from ? 1 : 0);
-    const float2 ml = __ldcg(a.part_ml + slot * a.unit + g);
-    const float2 v = __ldcg(reinterpret_cast<const float2*>(a.part_o + (slot * a.unit + g) * D + d));
-    const float now = fmaxf(mm, ml.x), ref = now == -INFINITY ? 0.f : now;
-    const float f = ex2(mm - ref), e = ex2(ml.x - ref);
-    mm = now;
-    ll = ll * f + ml.y * e;
-    ox = ox * f + v.x * e;
-    oy = oy * f + v.y * e;
+  auto slot = [&](int i) { return (((long long)(from + i) * units + hu) * 2 + (i == 0 ? 1 : 0)) * a.unit + g; };
+  float most = -INFINITY;
+  float2 mine = make_float2(-INFINITY, 0.f);
+  for (int i = threadIdx.x; i < n; i += 32 * PJ_WARPS) {
+    const float2 ml = __ldcg(a.part_ml + slot(i));
+    if (i == (int)threadIdx.x) mine = ml;
+    most = fmaxf(most, ml.x);
   }
-  const float f = ll == 0.f ? 0.f : 1.f / ll;
-  const long long at = (long long)__ldcg(&a.meta[p].seq) * a.q_heads + h0 + g;
-  *reinterpret_cast<uint32_t*>(a.out + at * D + d) = pack2(ox * f, oy * f);
-  if (a.lse && d == 0) a.lse[at] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * 0.693147180559945309f;
+#pragma unroll
+  for (int x = 16; x; x >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, x));
+  if (lane == 0) s_red[0][warp] = most;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < PJ_WARPS; ++w) most = fmaxf(most, s_red[0][w]);
+  const float ref = most == -INFINITY ? 0.f : most;
+  float ll = 0.f;
+  for (int i = threadIdx.x; i < n; i += 32 * PJ_WARPS) {
+    const float2 ml = i == (int)threadIdx.x ? mine : __ldcg(a.part_ml + slot(i));
+    const float f = ex2(ml.x - ref);
+    s_f[i] = f;
+    ll += f * ml.y;
+  }
+#pragma unroll
+  for (int x = 16; x; x >>= 1) ll += __shfl_xor_sync(0xffffffffu, ll, x);
+  if (lane == 0) s_red[1][warp] = ll;
+  __syncthreads();
+  ll = 0.f;
+#pragma unroll
+  for (int w = 0; w < PJ_WARPS; ++w) ll += s_red[1][w];
+  float o[V] = {};
+#pragma unroll 4
+  for (int i = warp; i < n; i += PJ_WARPS) {
+    const float f = s_f[i];
+    const float* src = a.part_o + slot(i) * D + lane * V;
+    if constexpr (V == 4) {
+      const float4 v = __ldcg(reinterpret_cast<const float4*>(src));
+      o[0] += f * v.x, o[1] += f * v.y, o[2] += f * v.z, o[3] += f * v.w;
+    } else {
+      const float2 v = __ldcg(reinterpret_cast<const float2*>(src));
+      o[0] += f * v.x, o[1] += f * v.y;
+    }
+  }
+#pragma unroll
+  for (int v = 0; v < V; ++v) s_o[warp][lane * V + v] = o[v];
+  __syncthreads();
+  if (threadIdx.x < D / 2) {
+    const int d = threadIdx.x * 2;
+    float x = 0.f, y = 0.f;
+#pragma unroll
+    for (int w = 0; w < PJ_WARPS; ++w) x += s_o[w][d], y += s_o[w][d + 1];
+    const float f = ll == 0.f ? 0.f : 1.f / ll;
+    const long long at = (long long)seq * a.q_heads + h0 + g;
+    *reinterpret_cast<uint32_t*>(a.out + at * D + d) = pack2(x * f, y * f);
+    if (a.lse && d == 0) a.lse[at] = ll == 0.f ? -INFINITY : (most + log2f(ll)) * LN2;
+  }
 }
 
 struct PagedPlan {
   int unit, groups, parts;
-  size_t meta, ml, bytes;
+  size_t meta, ml, o, bytes;
 };
 static PagedPlan paged_plan(const a3_handle* h) {
   PagedPlan p;
@@ -580,19 +719,20 @@ static PagedPlan paged_plan(const a3_handle* h) {
   const size_t slots = (size_t)p.parts * units * 2 * p.unit;
   p.meta = align_up(sizeof(PartMeta) * p.parts, 256);
   p.ml = align_up(slots * sizeof(float2), 256);
-  p.bytes = p.meta + p.ml + slots * h->m.head_dim * 4;
+  p.o = align_up(slots * h->m.head_dim * 4, 256);
+  p.bytes = p.meta + p.ml + p.o + (size_t)p.parts * units * PD_WARPS * p.unit * h->m.head_dim * 4;
   return p;
 }
 
-template <int D, bool F8, int NT>
+template <int D, bool F8, int NT, bool WHOLE>
 static int paged_launch(const a3_handle* h, const PagedAttnArgs& a, int units, cudaStream_t st) {
   static SmemAttrOnce once;
   using C = PagedCfg<D, F8, NT>;
-  A3_TRY(smem_attr_once(once, h->device, paged_attention_kernel<D, F8, NT>, C::SMEM));
-  A3_CUDA(launch_pdl(paged_attention_kernel<D, F8, NT>, dim3(a.parts * units), dim3(PD_THREADS), C::SMEM, st, a));
+  A3_TRY(smem_attr_once(once, h->device, paged_attention_kernel<D, F8, NT, WHOLE>, C::SMEM));
+  A3_CUDA(launch_pdl(paged_attention_kernel<D, F8, NT, WHOLE>, dim3(a.parts * units), dim3(C::THREADS), C::SMEM, st, a));
   A3_LAUNCHED();
   if (a.parts == 1) return A3_OK;  // every sequence ends in the part that it begins in
-  A3_CUDA(launch_pdl(paged_join_kernel<D>, dim3(a.parts - 1, units, a.unit), dim3(D / 2), 0, st, a));
+  A3_CUDA(launch_pdl(paged_join_kernel<D>, dim3(a.parts - 1, units, a.unit), dim3(32 * PJ_WARPS), a.parts * sizeof(float), st, a));
   return launched();
 }
 
@@ -607,6 +747,7 @@ extern "C" int a3_paged_attention(const a3_handle* h, const a3_paged_cache* cach
                                   void* ws, size_t ws_bytes, a3_stream stream) {
   if (!h || !cache || n_seqs < 0 || max_pages < 0 || !isfinite(scale)) return A3_EINVAL;
   A3_TRY(paged_cache_check(h, cache));
+  if ((long long)max_pages * cache->page_size > 0x7fff0000ll) return A3_EINVAL;  // slots are counted in 32 bits
   if (n_seqs == 0) return A3_OK;
   if ((!page_table && max_pages > 0) || !cache_len || !q_rows || !out || !ws) return A3_EINVAL;
   if (((uintptr_t)q_rows | (uintptr_t)out) & 15 || (uintptr_t)ws & 255) return A3_EINVAL;
@@ -627,6 +768,7 @@ extern "C" int a3_paged_attention(const a3_handle* h, const a3_paged_cache* cach
   a.meta = (PartMeta*)ws;
   a.part_ml = (float2*)((char*)ws + plan.meta);
   a.part_o = (float*)((char*)ws + plan.meta + plan.ml);
+  a.first_o = (float*)((char*)ws + plan.meta + plan.ml + plan.o);
   a.status = h->dev_status;
   cudaStream_t st = (cudaStream_t)stream;
   const int units = m.n_kv_heads * plan.groups;
@@ -634,7 +776,8 @@ extern "C" int a3_paged_attention(const a3_handle* h, const a3_paged_cache* cach
   const bool f8 = cache->type == A3_CACHE_E4M3;
   auto heads = [&](auto d, auto nt) {
     constexpr int DD = decltype(d)::value, N = decltype(nt)::value;
-    return f8 ? paged_launch<DD, true, N>(h, a, units, st) : paged_launch<DD, false, N>(h, a, units, st);
+    if (f8) return a.page_size % PagedCfg<DD, true, N>::KT ? paged_launch<DD, true, N, false>(h, a, units, st) : paged_launch<DD, true, N, true>(h, a, units, st);
+    return a.page_size % PagedCfg<DD, false, N>::KT ? paged_launch<DD, false, N, false>(h, a, units, st) : paged_launch<DD, false, N, true>(h, a, units, st);
   };
   using One = std::integral_constant<int, 1>;
   using Two = std::integral_constant<int, 2>;
