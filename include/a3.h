@@ -398,7 +398,7 @@ int a3_paged_append(const a3_handle* h, const a3_paged_cache* cache, const int32
  * token's own slot included; out: dev [n_seqs][Hq][D] bf16; lse_out: dev [n_seqs][Hq] fp32 natural-log row log-sum-exps of the scaled
  * logits, or NULL.  A sequence of length 0 (padding of a batch of fixed size) gives zeros and -inf.  A length below 0 or above
  * max_pages*page_size counts as 0, keys and values of a page outside [0, n_pages) count as zeros, and both set A3_DEV_BAD_POSITION.
- * max_pages*page_size is at most 2^31 - 2^16.  Lengths are read on the device only, so a captured call follows them.  The result is deterministic.
+ * A3_ETOOLARGE: max_pages*page_size above 2^31 - 2^16, or n_seqs times that above 2^34.  Lengths are read on the device only, so a captured call follows them.  The result is deterministic.
  * ws: dev, 256-byte aligned, a3_paged_attention_workspace_bytes(h) bytes, borrowed until the call's kernels have ended; needs
  * no clearing.  Two launches, no allocation, no synchronisation. */
 size_t a3_paged_attention_workspace_bytes(const a3_handle* h);

@@ -26,9 +26,9 @@
 
 namespace a3 {
 
-constexpr int PD_CTAS = 2;       // per SM
-constexpr int PD_WARPS = 4;       // of a CTA
+constexpr int PD_WARPS = 8;  // of a CTA, one per SM
 constexpr float LN2 = 0.693147180559945309f;
+constexpr int PD_LEAST = 2;  // tiles of a warp, before another part is begun
 constexpr float PD_SLACK = 8.f;  // see the running softmax
 
 struct PagedAttnArgs {
@@ -46,37 +46,21 @@ struct PagedAttnArgs {
   int q_heads, kv_heads, group, groups;  // groups: CTAs' head units per KV head, of `unit` query heads at most
   int unit, parts;
   // workspace
-  struct PartMeta* meta;  // [parts]
+  int4* meta;             // [parts]: what the join of part p does, see there
   float* part_o;          // [parts][units][2][unit][D]
   float2* part_ml;        // [parts][units][2][unit]
   float* first_o;         // [parts][units][warps][unit][D]: see below
   uint32_t* status;
 };
-// The sequence that a part begins with: its number, its first tile on the line and its tiles; the tiles on the line, the parts that share them.
-struct PartMeta {
-  long long first, tiles, total;
-  int seq, active;
-};
-
-// The line cut into `active` parts, the first ones a tile longer where it does not divide: one division, of 32 bits as a rule (one of 64
-// takes 200 clocks).
+// The line cut into `active` parts, the first ones a tile longer where it does not divide.
 struct Parts {
-  long long size, more;  // tiles of a part; parts that have one more
-  __device__ Parts(long long total, int active) {
-    if (total <= 0xffffffffll) {
-      const unsigned q = (unsigned)total / (unsigned)active;
-      size = q, more = (unsigned)total - q * (unsigned)active;
-    } else {
-      size = total / active, more = total - size * active;
-    }
+  unsigned size, more;  // tiles of a part; parts that have one more
+  __device__ Parts(unsigned total, unsigned active) : size(total / active), more(total - size * active) {}
+  __device__ unsigned begin(unsigned p) const { return p * size + min(p, more); }
+  __device__ int of(unsigned tile) const {
+    const unsigned longer = more * (size + 1);
+    return tile < longer ? tile / (size + 1) : more + (tile - longer) / size;
   }
-  __device__ long long begin(int p) const { return p * size + (p < more ? p : more); }
-  __device__ int of(long long tile) const {
-    const long long longer = more * (size + 1);
-    if (tile < longer) return quotient(tile, size + 1);
-    return (int)more + quotient(tile - longer, size);
-  }
-  __device__ static int quotient(long long a, long long b) { return a <= 0xffffffffll && b <= 0xffffffffll ? (int)((unsigned)a / (unsigned)b) : (int)(a / b); }
 };
 
 __device__ __forceinline__ uint32_t movmatrix(uint32_t x) {
@@ -104,6 +88,7 @@ __device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t two) {
 __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;\n" ::"r"(dst), "l"(src));
 }
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -129,18 +114,18 @@ struct PagedCfg {
 };
 
 struct SlotInfo {
-  long long first, tiles;  // of the sequence, on the line
-  int seq;                 // -1: empty
+  unsigned first, tiles;  // of the sequence, on the line
+  int seq;                // -1: empty
 };
 
 // WHOLE: a tile never crosses a page (page_size is a multiple of KT), so that its rows lie at one distance from each other.
 template <int D, bool F8, int NT, bool WHOLE>
-__global__ void __launch_bounds__(PagedCfg<D, F8, NT>::THREADS, PD_CTAS)
+__global__ void __launch_bounds__(PagedCfg<D, F8, NT>::THREADS, 1)
 paged_attention_kernel(const PagedAttnArgs a) {
   using C = PagedCfg<D, F8, NT>;
   constexpr int KT = C::KT, CH = C::CH, HN = C::HN, SUB = KT / 16, MT = D / 16, WARPS = C::WARPS;
   extern __shared__ __align__(1024) char smem[];
-  __shared__ long long s_scan[WARPS], s_warp_first[WARPS];
+  __shared__ unsigned s_scan[WARPS], s_warp_first[WARPS];
   __shared__ int s_warp_seq[WARPS], s_warp_len[WARPS];
   constexpr int TILES = 8, PAGES = 4, KEYS = WHOLE ? 1 : KT;
   __shared__ int4 s_tile[WARPS][TILES];  // of the tiles looked up, not yet computed: sequence, its length, tile in it, its first entry in its page
@@ -160,20 +145,50 @@ paged_attention_kernel(const PagedAttnArgs a) {
   pdl_launch_dependents();
   const float ks = F8 ? __ldcg(a.k_scale + kvh) : 1.f, vs = F8 ? __ldcg(a.v_scale + kvh) : 1.f;
 
-  // ---- the line: every thread adds up the tiles of a stretch of sequences
+  // What a warp will want once it knows its place is sent for into L2 while the lengths are on their way: every thread of the device
+  // one line of the page table and one of the queries.
+  {
+    const unsigned line = blockIdx.x * C::THREADS + threadIdx.x, per_seq = a.q_heads * (D / 64), s = line / per_seq;
+    if (line < (unsigned long long)a.n_seqs * a.max_pages / 32) prefetch_l2(a.table + line * 32ull);
+    if (s < (unsigned)a.n_seqs) prefetch_l2(a.q + s * a.q_stride + (line - s * per_seq) * 64);
+  }
+
+  // ---- the line: every thread adds up the tiles of a stretch of sequences; each warp for itself or, where they are many, all together
   const long long cap = (long long)a.max_pages * a.page_size;
   auto length = [&](int s) {
     const int n = __ldcg(a.lens + s);
     return n < 0 || n > cap ? 0 : n;
   };
-  const int per = (a.n_seqs + C::THREADS - 1) / C::THREADS, s0 = min(a.n_seqs, (int)threadIdx.x * per), s1 = min(a.n_seqs, s0 + per);
-  long long mine = 0;
+  const bool alone = a.n_seqs <= 256;
+  const int me = alone ? lane : threadIdx.x, per = (a.n_seqs + (alone ? 31 : C::THREADS - 1)) / (alone ? 32 : C::THREADS);
+  const int s0 = min(a.n_seqs, me * per), s1 = min(a.n_seqs, s0 + per);
+  unsigned mine = 0;
   int n0 = 0;  // the first of them
   for (int s = s0; s < s1; ++s) {
     const int n = length(s);
     if (s == s0) n0 = n;
     mine += (n + KT - 1) / KT;
-    if (n == 0 && part == 0) {  // nothing to attend to: no weight anywhere
+  }
+  unsigned upto = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const unsigned t = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += t;
+  }
+  unsigned total = __shfl_sync(0xffffffffu, upto, 31), before = upto - mine;
+  if (!alone) {
+    if (lane == 31) s_scan[warp] = upto;
+    __syncthreads();
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
+      if (w < warp) before += s_scan[w];
+      total += s_scan[w];
+    }
+  }
+  if (part == 0 && (!alone || warp == 0)) {  // sequences with nothing to attend to: no weight anywhere
+    for (int s = s0; s < s1; ++s) {
+      if (length(s) > 0) continue;
       if (__ldcg(a.lens + s) != 0 && hu == 0) atomicOr(a.status, A3_DEV_BAD_POSITION);
       for (int h = h0; h < h0 + hn; ++h) {
         uint4* o = reinterpret_cast<uint4*>(a.out + ((long long)s * a.q_heads + h) * D);
@@ -182,56 +197,56 @@ paged_attention_kernel(const PagedAttnArgs a) {
       }
     }
   }
-  long long upto = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long t = __shfl_up_sync(0xffffffffu, upto, o);
-    if (lane >= o) upto += t;
+  const int active = (int)min((total + PD_LEAST * WARPS - 1) / (PD_LEAST * WARPS), (unsigned)a.parts);
+  if (part >= active) {
+    if (hu == 0 && threadIdx.x == 0) a.meta[part] = make_int4(0, 0, 0, 0);
+    return;
   }
-  if (lane == 31) s_scan[warp] = upto;
-  __syncthreads();
-  long long total = 0, before = upto - mine;
-#pragma unroll
-  for (int w = 0; w < WARPS; ++w) {
-    if (w < warp) before += s_scan[w];
-    total += s_scan[w];
-  }
-  const long long wanted = (total + WARPS - 1) / WARPS;  // a tile for each warp at least
-  const int active = (int)(wanted < a.parts ? wanted : a.parts);
-  if (total == 0 && blockIdx.x == 0 && threadIdx.x == 0) a.meta[0].active = 0;
-  if (part >= active) return;
   const Parts parts(total, active);
-  const long long c0 = parts.begin(part), c1 = parts.begin(part + 1);
-  auto warp_begin = [&](int w) { return c0 + (c1 - c0) * w / WARPS; };
-  if (mine > 0) {
+  const unsigned c0 = parts.begin(part), c1 = parts.begin(part + 1);
+  auto warp_begin = [&](int w) { return c0 + (unsigned)((unsigned long long)(c1 - c0) * w / WARPS); };
+  const unsigned w0 = warp_begin(warp);
+  const int count = (int)(warp_begin(warp + 1) - w0);
+  // the sequence that this warp's stretch begins in: its number, its length, its first tile
+  int seq0 = 0, len0 = 0;
+  unsigned first0 = 0;
+  if (alone) {
     for (int s = s0; s < s1; ++s) {
-      const int n = s == s0 ? n0 : length(s), tiles = (n + KT - 1) / KT;
+      const int n = s == s0 ? n0 : length(s);
+      const unsigned tiles = (n + KT - 1) / KT;
+      if (w0 >= before && w0 < before + tiles) seq0 = s, len0 = n, first0 = before;
+      before += tiles;
+    }
+    const int who = __ffs(__ballot_sync(0xffffffffu, len0 > 0)) - 1;  // none where the stretch is empty and at the line's end
+    seq0 = __shfl_sync(0xffffffffu, seq0, who & 31), len0 = __shfl_sync(0xffffffffu, len0, who & 31), first0 = __shfl_sync(0xffffffffu, first0, who & 31);
+  } else {
+    for (int s = s0; s < s1; ++s) {
+      const int n = s == s0 ? n0 : length(s);
+      const unsigned tiles = (n + KT - 1) / KT;
       for (int w = 0; w < WARPS; ++w) {
-        const long long b = warp_begin(w);
+        const unsigned b = warp_begin(w);
         if (b >= before && b < before + tiles) s_warp_seq[w] = s, s_warp_first[w] = before, s_warp_len[w] = n;
       }
       before += tiles;
     }
+    __syncthreads();
+    seq0 = s_warp_seq[warp], len0 = s_warp_len[warp], first0 = s_warp_first[warp];
   }
-  __syncthreads();
+  __syncthreads();  // s_info
 
   // ---- this warp's stretch
-  const long long w0 = warp_begin(warp), w1 = warp_begin(warp + 1);
-  const int count = (int)(w1 - w0);
-  if (hu == 0 && threadIdx.x == 0)
-    a.meta[part] = PartMeta{s_warp_first[0], (s_warp_len[0] + KT - 1) / KT, total, s_warp_seq[0], active};
   if (count > 0) {
     const long long entry = (long long)a.kv_heads * C::ROWB;
     const char *k_base = a.k_pages + (long long)kvh * C::ROWB + lane % CH * 16, *v_base = a.v_pages + (long long)kvh * C::ROWB + lane % CH * 16;
     const long long step = 32 / CH * entry;
     constexpr int RPI = 32 / CH;            // rows that a warp copies with one instruction
-    long long cfirst = s_warp_first[warp];  // first tile of the sequence that is computed
+    unsigned cfirst = first0;               // first tile of the sequence that is computed
 
     // Queries of a sequence, one head in eight for each group of four lanes, raw.  Those of the next one are fetched while a sequence is
     // computed (where the registers suffice), the first ones before any key: behind the copies under way a load takes 2 us.
     uint32_t qf[MT][NT][2], qn[MT][NT][2];
     uint32_t(&qr)[MT][NT][2] = NT == 1 ? qn : qf;
-    int q_seq = s_warp_seq[warp];
+    int q_seq = seq0;
     auto load_q = [&] {
       const bf16* q = a.q + q_seq * a.q_stride;
 #pragma unroll
@@ -247,7 +262,7 @@ paged_attention_kernel(const PagedAttnArgs a) {
 
     // Three steps of a tile, each in its own turn: its pages are looked up, three turns later its rows are copied, two turns after that it
     // is computed.  Pages and rows come by asynchronous copies, so that no turn waits for an access that it makes itself.
-    int xs = q_seq, xn = s_warp_len[warp], xt = (int)(w0 - s_warp_first[warp]), xp = xt * KT / a.page_size, xe = xt * KT - xp * a.page_size;
+    int xs = seq0, xn = len0, xt = (int)(w0 - first0), xp = xt * KT / a.page_size, xe = xt * KT - xp * a.page_size;
     int x_left = count, x_next = xs + 1 < a.n_seqs ? length(xs + 1) : 0;
     auto look_up = [&](int j) {
       if (x_left <= 0) return;
@@ -314,26 +329,24 @@ paged_attention_kernel(const PagedAttnArgs a) {
     };
 
     float o[MT][NT][4], m[NT][2], l[NT][2], cq[NT][2];
-    load_q();
-#pragma unroll
+#pragma unroll 1
     for (int j = 0; j < 3; ++j) look_up(j);
     cp_async_commit();
+    load_q();
     cp_async_wait<0>();
     __syncwarp();
-    auto turn = [&](int j) {
-      copy(j);
-      look_up(j + 3);
-      cp_async_commit();
-    };
     static_assert(C::STAGES == 3, "two turns between the copy and its use, three between look-up and copy");
-    turn(0);
-    __syncwarp();  // a look-up may take the place of the page that another lane has just read
-    turn(1);
-    __syncwarp();
     bool fresh = true;
     int piece0 = 0;
-    for (int i = 0; i < count; ++i) {
-      turn(i + 2);
+    // the first two turns only copy: what runs once should not be there a second time, its instructions come cold from L2
+    for (int i = -2; i < count; ++i) {
+      copy(i + 2);
+      look_up(i + 5);
+      cp_async_commit();
+      if (i < 0) {
+        __syncwarp();  // a look-up may take the place of the page that another lane has just read
+        continue;
+      }
       const int4 tile = s_tile[warp][i % TILES];
       const int cs = tile.x, cn = tile.y, ct = tile.z;
       if (fresh) {  // a sequence, or what is left of one, begins
@@ -573,45 +586,63 @@ paged_attention_kernel(const PagedAttnArgs a) {
               }
               if (lane / 4 == 0) s_m[info][h] = m[nt][e], s_l[info][h] = l[nt][e];
             }
-          if (lane == 0) s_info[info] = SlotInfo{cfirst, tiles, cs};
+          if (lane == 0) s_info[info] = SlotInfo{cfirst, (unsigned)tiles, cs};
         }
         fresh = true;
         if (ct == tiles - 1) cfirst += tiles;
       }
     }
   }
+  if (hu == 0 && threadIdx.x == 0) {  // first0 and len0 are of the sequence that the part begins with
+    const int from = first0 < c0 ? parts.of(first0) : part, to = parts.of(first0 + (unsigned)(len0 + KT - 1) / KT - 1);
+    a.meta[part] = make_int4(seq0, from, from == part - 1 ? to - from + 1 : 0, 0);
+  }
   __syncthreads();
 
   // ---- what the warps hold of one sequence, merged
-  for (int i0 = 0; i0 < 2 * WARPS; ++i0) {
-    const SlotInfo info = s_info[i0];
-    if (info.seq < 0) continue;
-    bool first_of = true;
-    for (int i = 0; i < i0; ++i) first_of = first_of && s_info[i].seq != info.seq;
-    if (!first_of) continue;
-    const bool began = info.first < c0, goes_on = info.first + info.tiles > c1;
-    const long long slot = ((long long)part * units + hu) * 2 + (began ? 0 : 1);
+  int seqs[2 * WARPS];
+#pragma unroll
+  for (int i = 0; i < 2 * WARPS; ++i) seqs[i] = s_info[i].seq;
+  unsigned left = 0;
+#pragma unroll
+  for (int i = 0; i < 2 * WARPS; ++i) left |= (seqs[i] >= 0) << i;
+  while (left) {
+    const SlotInfo info = s_info[__ffs(left) - 1];
     unsigned members = 0;
 #pragma unroll
-    for (int i = 0; i < 2 * WARPS; ++i) members |= (s_info[i].seq == info.seq) << i;
+    for (int i = 0; i < 2 * WARPS; ++i) members |= (seqs[i] == info.seq) << i;
+    left &= ~members;
+    const bool began = info.first < c0, goes_on = info.first + info.tiles > c1;
+    const long long slot = ((long long)part * units + hu) * 2 + (began ? 0 : 1);
     for (int x = threadIdx.x; x < hn * (D / 4); x += C::THREADS) {
       const int h = x / (D / 4), d = x % (D / 4) * 4;
-      float f[2 * WARPS], mm = -INFINITY, ll = 0.f;
+      // the warps' last pieces lie in shared memory, all read at once whether they belong to this sequence or not; first pieces are rare
+      float f[WARPS], mm = -INFINITY, ll = 0.f;
+      float4 v[WARPS];
 #pragma unroll
-      for (int i = 0; i < 2 * WARPS; ++i) {
-        f[i] = members >> i & 1 ? s_m[i][h] : -INFINITY;
-        mm = fmaxf(mm, f[i]);
+      for (int w = 0; w < WARPS; ++w) {
+        f[w] = s_m[2 * w + 1][h];
+        v[w] = *reinterpret_cast<const float4*>(smem + w * C::RING + C::out_at(h, d) * 4);
       }
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) {
+        if (!(members >> (2 * w + 1) & 1)) f[w] = -INFINITY;
+        mm = fmaxf(mm, f[w]);
+      }
+      for (unsigned b = members & 0x55555555u; b; b &= b - 1) mm = fmaxf(mm, s_m[__ffs(b) - 1][h]);
       const float ref = mm == -INFINITY ? 0.f : mm;
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      auto add = [&](float g, float l, const float4& y) {
+        ll += g * l;
+        o.x += g * y.x, o.y += g * y.y, o.z += g * y.z, o.w += g * y.w;
+      };
 #pragma unroll
-      for (int i = 0; i < 2 * WARPS; ++i)
-        if (members >> i & 1) {
-          const float g = ex2(f[i] - ref);
-          const float4 v = *reinterpret_cast<const float4*>((i & 1 ? reinterpret_cast<const float*>(smem + i / 2 * C::RING) : first_o + i / 2 * a.unit * D) + C::out_at(h, d));
-          ll += g * s_l[i][h];
-          o.x += g * v.x, o.y += g * v.y, o.z += g * v.z, o.w += g * v.w;
-        }
+      for (int w = 0; w < WARPS; ++w)
+        if (members >> (2 * w + 1) & 1) add(ex2(f[w] - ref), s_l[2 * w + 1][h], v[w]);
+      for (unsigned b = members & 0x55555555u; b; b &= b - 1) {
+        const int i = __ffs(b) - 1;
+        add(ex2(s_m[i][h] - ref), s_l[i][h], *reinterpret_cast<const float4*>(first_o + i / 2 * a.unit * D + C::out_at(h, d)));
+      }
       if (!began && !goes_on) {
         const float g = ll == 0.f ? 0.f : 1.f / ll;
         const long long at = (long long)info.seq * a.q_heads + h0 + h;
@@ -625,8 +656,9 @@ paged_attention_kernel(const PagedAttnArgs a) {
   }
 }
 
-// Block (p, unit, head): the sequence that part p begins with, if it began in the part before, from all parts that hold some of it.
-// A warp's lanes cover the head dimension; the warps take parts in turn.
+// Block (p, unit, head): the sequence that part p begins with, if it began in the part before, from all parts that hold some of it:
+// meta[p] = (sequence, first of those parts, how many, -), none where there is nothing to join.  A warp's lanes cover the head dimension;
+// the warps take parts in turn.
 constexpr int PJ_WARPS = 4;
 template <int D>
 __global__ void __launch_bounds__(32 * PJ_WARPS)
@@ -634,20 +666,23 @@ paged_join_kernel(const PagedAttnArgs a) {
   constexpr int V = D / 32;
   extern __shared__ float s_f[];  // [parts] weights
   __shared__ float s_red[2][PJ_WARPS], s_o[PJ_WARPS][D];
-  pdl_wait();
-  pdl_launch_dependents();
   const int p = blockIdx.x + 1, hu = blockIdx.y, g = blockIdx.z, units = a.kv_heads * a.groups, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int kvh = hu / a.groups, h0 = kvh * a.group + hu % a.groups * a.unit, hn = min(a.unit, (kvh + 1) * a.group - h0);
+  pdl_wait();
+  pdl_launch_dependents();
   if (g >= hn) return;
-  // all at once; what part p says is right only where there is such a part
-  const int active = __ldcg(&a.meta[0].active), seq = __ldcg(&a.meta[p].seq);
-  const long long total = __ldcg(&a.meta[p].total), first = __ldcg(&a.meta[p].first), tiles = __ldcg(&a.meta[p].tiles);
-  if (p >= active) return;
-  const Parts parts(total, active);
-  if (first >= parts.begin(p)) return;
-  const int from = parts.of(first), n = parts.of(first + tiles - 1) - from + 1;
-  if (from != p - 1) return;
-  auto slot = [&](int i) { return (((long long)(from + i) * units + hu) * 2 + (i == 0 ? 1 : 0)) * a.unit + g; };
+  const int4 meta = __ldcg(a.meta + p);
+  const int seq = meta.x, from = meta.y, n = meta.z;
+  if (n == 0) return;
+  constexpr int EARLY = 8;  // parts of a warp whose outputs are sent for before their weights are known
+  // the first part holds the sequence's beginning in its second place, the others hold it in their first
+  const int at0 = (from * units + hu) * 2 * a.unit + g, stride = units * 2 * a.unit;
+  auto slot = [&](int i) { return at0 + i * stride + (i == 0 ? a.unit : 0); };
+  using Vec = std::conditional_t<V == 4, float4, float2>;
+  Vec early[EARLY];
+#pragma unroll
+  for (int k = 0; k < EARLY; ++k)
+    if (warp + k * PJ_WARPS < n) early[k] = __ldcg(reinterpret_cast<const Vec*>(a.part_o + (long long)slot(warp + k * PJ_WARPS) * D + lane * V));
   float most = -INFINITY;
   float2 mine = make_float2(-INFINITY, 0.f);
   for (int i = threadIdx.x; i < n; i += 32 * PJ_WARPS) {
@@ -677,18 +712,15 @@ paged_join_kernel(const PagedAttnArgs a) {
 #pragma unroll
   for (int w = 0; w < PJ_WARPS; ++w) ll += s_red[1][w];
   float o[V] = {};
+  auto add = [&](const Vec& v, float f) {
+    o[0] += f * v.x, o[1] += f * v.y;
+    if constexpr (V == 4) o[2] += f * v.z, o[3] += f * v.w;
+  };
+#pragma unroll
+  for (int k = 0; k < EARLY; ++k)
+    if (warp + k * PJ_WARPS < n) add(early[k], s_f[warp + k * PJ_WARPS]);
 #pragma unroll 4
-  for (int i = warp; i < n; i += PJ_WARPS) {
-    const float f = s_f[i];
-    const float* src = a.part_o + slot(i) * D + lane * V;
-    if constexpr (V == 4) {
-      const float4 v = __ldcg(reinterpret_cast<const float4*>(src));
-      o[0] += f * v.x, o[1] += f * v.y, o[2] += f * v.z, o[3] += f * v.w;
-    } else {
-      const float2 v = __ldcg(reinterpret_cast<const float2*>(src));
-      o[0] += f * v.x, o[1] += f * v.y;
-    }
-  }
+  for (int i = warp + EARLY * PJ_WARPS; i < n; i += PJ_WARPS) add(__ldcg(reinterpret_cast<const Vec*>(a.part_o + (long long)slot(i) * D + lane * V)), s_f[i]);
 #pragma unroll
   for (int v = 0; v < V; ++v) s_o[warp][lane * V + v] = o[v];
   __syncthreads();
@@ -714,10 +746,10 @@ static PagedPlan paged_plan(const a3_handle* h) {
   p.unit = group <= 8 ? group : 16;  // query heads that one pass over the keys serves
   p.groups = cdiv(group, p.unit);
   const int units = h->m.n_kv_heads * p.groups;
-  p.parts = h->sm_count * PD_CTAS / units;
+  p.parts = h->sm_count / units;
   if (p.parts < 1) p.parts = 1;
   const size_t slots = (size_t)p.parts * units * 2 * p.unit;
-  p.meta = align_up(sizeof(PartMeta) * p.parts, 256);
+  p.meta = align_up(sizeof(int4) * p.parts, 256);
   p.ml = align_up(slots * sizeof(float2), 256);
   p.o = align_up(slots * h->m.head_dim * 4, 256);
   p.bytes = p.meta + p.ml + p.o + (size_t)p.parts * units * PD_WARPS * p.unit * h->m.head_dim * 4;
@@ -747,7 +779,9 @@ extern "C" int a3_paged_attention(const a3_handle* h, const a3_paged_cache* cach
                                   void* ws, size_t ws_bytes, a3_stream stream) {
   if (!h || !cache || n_seqs < 0 || max_pages < 0 || !isfinite(scale)) return A3_EINVAL;
   A3_TRY(paged_cache_check(h, cache));
-  if ((long long)max_pages * cache->page_size > 0x7fff0000ll) return A3_EINVAL;  // slots are counted in 32 bits
+  // slots of a sequence and tiles of all sequences (16 slots at least) are counted in 32 bits
+  const unsigned long long slots = (unsigned long long)max_pages * cache->page_size;
+  if (slots > 0x7fff0000ull || (n_seqs > 0 && slots > (1ull << 34) / n_seqs)) return A3_ETOOLARGE;
   if (n_seqs == 0) return A3_OK;
   if ((!page_table && max_pages > 0) || !cache_len || !q_rows || !out || !ws) return A3_EINVAL;
   if (((uintptr_t)q_rows | (uintptr_t)out) & 15 || (uintptr_t)ws & 255) return A3_EINVAL;
@@ -765,7 +799,7 @@ extern "C" int a3_paged_attention(const a3_handle* h, const a3_paged_cache* cach
   a.out = (bf16*)out, a.lse = lse_out;
   a.q_heads = m.n_q_heads, a.kv_heads = m.n_kv_heads, a.group = m.n_q_heads / m.n_kv_heads;
   a.unit = plan.unit, a.groups = plan.groups, a.parts = plan.parts;
-  a.meta = (PartMeta*)ws;
+  a.meta = (int4*)ws;
   a.part_ml = (float2*)((char*)ws + plan.meta);
   a.part_o = (float*)((char*)ws + plan.meta + plan.ml);
   a.first_o = (float*)((char*)ws + plan.meta + plan.ml + plan.o);
