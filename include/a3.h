@@ -379,7 +379,8 @@ typedef struct {
 
 /* Rows into a paged cache, rotated on the way: row r goes to slot row_slot[r] of sequence row_seq[r],
  *   k' = R(pos) k_rows[r], v' = v_rows[r], q_out[r] = R(pos) q_rows[r],   pos = row_pos ? row_pos[r] : row_slot[r]
- * in fp32 arithmetic, rounded once to the type that is stored (e4m3: k'/k_scale[head], beyond +-448 the largest value; NaN stays NaN).
+ * in fp32 arithmetic, rounded once to the type that is stored (e4m3: k' times the fp32 reciprocal of
+ * k_scale[head], a positive number whose reciprocal is finite; beyond +-448 the largest value; NaN stays NaN).
  * pos may be negative (turns back) and differs from the slot in a cache that a3_evict_layer has shortened, or
  * where a stored chunk's keys at local positions are recovered (Eq. 2: pos = the chunk's offset for every row).  rotate = 0: keys and
  * queries are copied as they are (rows of a fused cache).  q_rows and q_out: both NULL where there are no queries to rotate; q_out may be

@@ -443,84 +443,103 @@ class A3:
                                       _ptr(ws), ws.numel(), _stream()), "a3_first_token")
         return logits, token
 
-    # ---- decoding on paged caches
-    def _indices(self, where, *tensors):
-        for t in tensors:
-            _need(t.dtype == torch.int32 and t.device == self.device and t.is_contiguous(), where + ": int32 indices on the engine's device")
+    # ---- decoding on paged caches (these calls are short on the device: each check is made once, and no text is built before it is needed)
+    def _ints(self, where, t, shape):
+        """Address of an int32 tensor of this shape on the engine's device."""
+        if t.dtype is not torch.int32 or t.shape != shape or t.device != self.device or not t.is_contiguous():
+            raise A3Error(-1, where + ": int32 indices on the engine's device")
+        return t.data_ptr()
 
-    def _rows(self, where, t, heads, n):
-        """Elements between the rows of t [n][heads][D], whose heads lie next to each other."""
-        m = self.shape
-        _need(t.dtype == torch.bfloat16 and t.shape == (n, heads, m.head_dim) and t.device == self.device, where)
-        sr, sh, se = t.stride()
-        _need(n == 0 or (se == 1 and (sh == m.head_dim or heads == 1)), where)
-        return sr if n > 1 else heads * m.head_dim
+    def _rows(self, where, t, shape):
+        """Address of bf16 rows of this shape [n][heads][D], whose heads lie next to each other, and the elements between them."""
+        if t.dtype is not torch.bfloat16 or t.shape != shape or t.device != self.device:
+            raise A3Error(-1, where + ": bf16 rows on the engine's device")
+        n, heads, d = shape
+        row, head, one = t.stride()
+        if n > 0 and (one != 1 or (head != d and heads > 1)):
+            raise A3Error(-1, where + ": the heads of a row lie next to each other")
+        return t.data_ptr(), row if n > 1 else heads * d
 
     def _paged(self, where, cache, page_table):
         m = self.shape
-        _need(cache.n_kv_heads == m.n_kv_heads and cache.head_dim == m.head_dim and cache.device == self.device, where + ": the cache is another model's")
-        self._indices(where, page_table)
-        _need(page_table.dim() == 2, where + ": page table")
+        if cache.n_kv_heads != m.n_kv_heads or cache.head_dim != m.head_dim or cache.device != self.device or page_table.dim() != 2:
+            raise A3Error(-1, where + ": cache of another model or device, or no page table")
+        return page_table.shape
 
     def paged_append(self, cache: PagedCache, page_table, row_seq, row_slot, k_rows, v_rows, q_rows=None, row_pos=None, rotate=True, q_out=None):
         """a3_paged_append; page_table [n_seqs][max_pages], rows [M][heads][D] (columns of a wider buffer will do); returns q_out or None."""
-        where, m, M = "a3_paged_append", self.shape, row_seq.shape[0]
-        self._paged(where, cache, page_table)
-        self._indices(where, row_seq, row_slot, *(() if row_pos is None else (row_pos,)))
-        _need(row_seq.shape == row_slot.shape == (M,) and (row_pos is None or row_pos.shape == (M,)), where + ": rows")
-        ks, vs = self._rows(where + ": k_rows", k_rows, m.n_kv_heads, M), self._rows(where + ": v_rows", v_rows, m.n_kv_heads, M)
+        where, m = "a3_paged_append", self.shape
+        table_shape = n_seqs, max_pages = self._paged(where, cache, page_table)
+        rows = row_seq.shape
+        if len(rows) != 1:
+            raise A3Error(-1, where + ": row_seq")
+        M, D = rows[0], m.head_dim
+        kv_shape = (M, m.n_kv_heads, D)
+        k, ks = self._rows(where, k_rows, kv_shape)
+        v, vs = self._rows(where, v_rows, kv_shape)
+        q = out = None
         qs = os = 0
         if q_rows is not None:
-            qs = self._rows(where + ": q_rows", q_rows, m.n_q_heads, M)
+            q_shape = (M, m.n_q_heads, D)
+            q, qs = self._rows(where, q_rows, q_shape)
             if q_out is None:
-                q_out = torch.empty((M, m.n_q_heads, m.head_dim), dtype=torch.bfloat16, device=self.device)
-            os = self._rows(where + ": q_out", q_out, m.n_q_heads, M)
-        _need(q_rows is not None or q_out is None, where + ": q_out without q_rows")
-        _check(_load().a3_paged_append(self._h, cache._ref, page_table.data_ptr(), page_table.shape[0], page_table.shape[1], row_seq.data_ptr(),
-                                       row_slot.data_ptr(), None if row_pos is None else row_pos.data_ptr(), 1 if rotate else 0,
-                                       None if q_rows is None else q_rows.data_ptr(), qs, k_rows.data_ptr(), ks, v_rows.data_ptr(), vs, M,
-                                       None if q_out is None else q_out.data_ptr(), os, _stream()), where)
+                q_out = q_rows.new_empty(q_shape)
+            out, os = self._rows(where, q_out, q_shape)
+        elif q_out is not None:
+            raise A3Error(-1, where + ": q_out without q_rows")
+        status = _load().a3_paged_append(self._h, cache._ref, self._ints(where, page_table, table_shape), n_seqs, max_pages, self._ints(where, row_seq, rows),
+                                         self._ints(where, row_slot, rows), None if row_pos is None else self._ints(where, row_pos, rows),
+                                         1 if rotate else 0, q, qs, k, ks, v, vs, M, out, os, _stream())
+        if status != A3_OK:
+            raise A3Error(status, where)
         return q_out
 
     def paged_attention(self, cache: PagedCache, page_table, cache_len, q_rows, scale=None, out=None, want_lse=False):
         """a3_paged_attention; returns (out [n_seqs][Hq][D], lse [n_seqs][Hq] or None).  The workspace is allocated by torch for
         this call alone, so that calls on several streams, or captured into several graphs, share none."""
-        where, m, n = "a3_paged_attention", self.shape, cache_len.shape[0]
-        lib = _load()
-        self._paged(where, cache, page_table)
-        self._indices(where, cache_len)
-        _need(cache_len.dim() == 1 and page_table.shape[0] == n, where + ": sequences")
-        qs = self._rows(where + ": q_rows", q_rows, m.n_q_heads, n)
+        where, m, lib = "a3_paged_attention", self.shape, _load()
+        table_shape = n, max_pages = self._paged(where, cache, page_table)
+        heads = m.n_q_heads
+        shape = (n, heads, m.head_dim)
+        q, qs = self._rows(where, q_rows, shape)
         if out is None:
-            out = torch.empty((n, m.n_q_heads, m.head_dim), dtype=torch.bfloat16, device=self.device)
-        _need(out.dtype == torch.bfloat16 and out.shape == (n, m.n_q_heads, m.head_dim) and out.is_contiguous() and out.device == self.device, where + ": out")
-        lse = torch.empty((n, m.n_q_heads), dtype=torch.float32, device=self.device) if want_lse else None
+            out = torch.empty_like(q_rows, memory_format=torch.contiguous_format)
+        elif out.dtype is not torch.bfloat16 or out.shape != shape or not out.is_contiguous() or out.device != self.device:
+            raise A3Error(-1, where + ": out")
+        lse = q_rows.new_empty((n, heads), dtype=torch.float32) if want_lse else None
         nbytes = lib.a3_paged_attention_workspace_bytes(self._h)
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-        _check(lib.a3_paged_attention(self._h, cache._ref, page_table.data_ptr(), n, page_table.shape[1], cache_len.data_ptr(), q_rows.data_ptr(), qs,
-                                      m.head_dim ** -0.5 if scale is None else scale, out.data_ptr(), None if lse is None else lse.data_ptr(),
-                                      ws.data_ptr(), nbytes, _stream()), where)
+        ws = q_rows.new_empty(nbytes, dtype=torch.uint8)
+        status = lib.a3_paged_attention(self._h, cache._ref, self._ints(where, page_table, table_shape), n, max_pages, self._ints(where, cache_len, (n,)), q, qs,
+                                        m.head_dim ** -0.5 if scale is None else scale, out.data_ptr(), None if lse is None else lse.data_ptr(),
+                                        ws.data_ptr(), nbytes, _stream())
+        if status != A3_OK:
+            raise A3Error(status, where)
         return out, lse
 
     def token_logprobs(self, logits, targets=None, n_top=0):
         """a3_token_logprobs on logits [M][vocab] (fp32, bf16 or fp16; rows may be apart); returns (logprob [M] or None without targets,
         entropy [M], top_ids [M][n_top] and top_logprobs [M][n_top], or None)."""
         where = "a3_token_logprobs"
-        _need(logits.dim() == 2 and logits.dtype in _LOGIT_TYPES and logits.device == self.device, where + ": logits")
+        kind = _LOGIT_TYPES.get(logits.dtype)
+        if kind is None or logits.dim() != 2 or logits.device != self.device:
+            raise A3Error(-1, where + ": logits")
         M, vocab = logits.shape
-        _need(vocab > 0 and (logits.stride(1) == 1 or vocab == 1), where + ": logits of a row lie next to each other")
-        dev, logprob, ids, lps = self.device, None, None, None
+        row, one = logits.stride()
+        if vocab == 0 or (one != 1 and vocab > 1):
+            raise A3Error(-1, where + ": logits of a row lie next to each other")
+        logprob = ids = lps = t = None
         if targets is not None:
-            self._indices(where, targets)
-            _need(targets.shape == (M,), where + ": targets")
-            logprob = torch.empty(M, dtype=torch.float32, device=dev)
-        entropy = torch.empty(M, dtype=torch.float32, device=dev)
+            t = self._ints(where, targets, (M,))
+            logprob = logits.new_empty(M, dtype=torch.float32)
+        entropy = torch.empty_like(logprob) if t else logits.new_empty(M, dtype=torch.float32)
         if n_top > 0:
-            ids, lps = torch.empty((M, n_top), dtype=torch.int32, device=dev), torch.empty((M, n_top), dtype=torch.float32, device=dev)
-        _check(_load().a3_token_logprobs(self._h, logits.data_ptr(), _LOGIT_TYPES[logits.dtype], logits.stride(0) if M > 1 else vocab, M, vocab,
-                                         None if targets is None else targets.data_ptr(), n_top, None if logprob is None else logprob.data_ptr(),
-                                         entropy.data_ptr(), None if ids is None else ids.data_ptr(), None if lps is None else lps.data_ptr(),
-                                         _stream()), where)
+            lps = logits.new_empty((M, n_top), dtype=torch.float32)
+            ids = torch.empty_like(lps, dtype=torch.int32)
+        status = _load().a3_token_logprobs(self._h, logits.data_ptr(), kind, row if M > 1 else vocab, M, vocab, t, n_top,
+                                           None if logprob is None else logprob.data_ptr(), entropy.data_ptr(),
+                                           None if ids is None else ids.data_ptr(), None if lps is None else lps.data_ptr(), _stream())
+        if status != A3_OK:
+            raise A3Error(status, where)
         return logprob, entropy, ids, lps
 
     def make_request(self, chunks, n_chunks, max_chunk_len, n_ctx, n_question, x0, k_fused, v_fused, ratio=0.15,

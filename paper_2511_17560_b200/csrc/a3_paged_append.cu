@@ -1,9 +1,8 @@
 // Rows into a paged cache (a3_paged_append): keys rotated to their positions, values as they are, queries rotated beside them.
 //
-// A row is cut into units of 16 elements of one head that rotate among themselves: for pairs (i, i + D/2) the two 16-byte vectors at
-// 8j and 8j + D/2, for pairs (2i, 2i+1) two neighbouring vectors.  One thread moves one unit: its two loads do not depend on
-// where the row goes, so they are on their way while the page is looked up.  Bound by HBM where rows are many and by
-// the chain slot -> page -> store where they are few.
+// A row is cut into units of 16 elements of one head: the two 16-byte vectors at 8j and 8j + D/2, which with pairs (i, i + D/2) rotate
+// among themselves and with pairs (2i, 2i+1) each within itself.  One thread moves the units j of `HEADS` heads of a row, which share
+// the cosines and sines: its loads do not depend on where the row goes, so they are on their way while the page is looked up.
 #include <cuda_fp8.h>
 
 #include "a3_internal.cuh"
@@ -12,6 +11,11 @@
 namespace a3 {
 
 constexpr int PA_THREADS = 256;
+#ifndef PA_MIN
+#define PA_MIN 1
+#define PA_HEADS 4
+#endif
+constexpr int PA_ONE = 2048;  // units per SM up to which a thread moves one head
 
 struct AppendArgs {
   char *k_pages, *v_pages;
@@ -30,81 +34,99 @@ struct AppendArgs {
   uint32_t* status;
 };
 
-__device__ __forceinline__ uint2 pack8_e4m3(const float* f, float scale) {
+// One rounding to 8 bits, from the rotated fp32 value by the reciprocal of the scale (2^-23 off the quotient at most: a true division of every
+// element would take more instructions than all else); beyond the largest value: the largest value.
+__device__ __forceinline__ uint2 pack8_e4m3(const float* f, float by) {
   uint32_t h[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {  // one rounding, from the rotated fp32 value; beyond the largest value: the largest value
-    float2 t = make_float2(__fdiv_rn(f[2 * i], scale), __fdiv_rn(f[2 * i + 1], scale));
-    h[i] = __nv_cvt_float2_to_fp8x2(t, __NV_SATFINITE, __NV_E4M3);
-  }
+  for (int i = 0; i < 4; ++i) h[i] = __nv_cvt_float2_to_fp8x2(make_float2(f[2 * i] * by, f[2 * i + 1] * by), __NV_SATFINITE, __NV_E4M3);
   return make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
 }
 
-template <int D, int LAYOUT, bool F8>
-__global__ void __launch_bounds__(PA_THREADS)
+template <int D, int LAYOUT, bool F8, int HEADS>
+__global__ void __launch_bounds__(PA_THREADS, PA_MIN)
 paged_append_kernel(const AppendArgs a) {
   pdl_wait();
   pdl_launch_dependents();
   constexpr int UPH = D / 16;  // units per head
-  const int heads = a.q_heads + 2 * a.kv_heads;
-  const unsigned upr = (unsigned)heads * UPH;
+  const int heads = a.q_heads + 2 * a.kv_heads, stride = (heads + HEADS - 1) / HEADS;  // of the thread's heads
+  const unsigned upr = (unsigned)stride * UPH;
   const unsigned long long idx = (unsigned long long)blockIdx.x * PA_THREADS + threadIdx.x;
-  const long long r = (long long)(idx / upr);
+  const int r = (int)(HEADS == 1 ? idx / upr : (unsigned)idx / upr);  // with several heads a launch has less than 2^32 threads
   if (r >= a.M) return;
-  const int u = (int)(idx % upr), j = u % UPH;
-  int head = u / UPH;
-  const int what = head < a.q_heads ? 0 : head < a.q_heads + a.kv_heads ? 1 : 2;  // q, k, v
-  if (what) head -= a.q_heads + (what == 2 ? a.kv_heads : 0);
-  const bf16* src = (what == 0 ? a.q + r * a.q_stride : what == 1 ? a.k + r * a.k_stride : a.v + r * a.v_stride) + head * D;
-  const bool halves = LAYOUT == 0 && what != 2;
-  const int lo = halves ? 8 * j : 16 * j, hi = halves ? lo + D / 2 : lo + 8;
-  const uint4 x0 = __ldcs(reinterpret_cast<const uint4*>(src + lo)), x1 = __ldcs(reinterpret_cast<const uint4*>(src + hi));
-
+  const int u = (int)(idx - (unsigned long long)r * upr), j = u % UPH, h0 = u / UPH;
+  uint4 x[HEADS][2];
+#pragma unroll
+  for (int i = 0; i < HEADS; ++i) {
+    const int h = h0 + i * stride;
+    if (h < heads) {
+      const bf16* src = h < a.q_heads ? a.q + r * a.q_stride + h * D
+                        : h < a.q_heads + a.kv_heads ? a.k + r * a.k_stride + (h - a.q_heads) * D : a.v + r * a.v_stride + (h - a.q_heads - a.kv_heads) * D;
+      x[i][0] = __ldcs(reinterpret_cast<const uint4*>(src + 8 * j));
+      x[i][1] = __ldcs(reinterpret_cast<const uint4*>(src + 8 * j + D / 2));
+    }
+  }
   const int seq = __ldcg(a.row_seq + r), slot = __ldcg(a.row_slot + r);  // what a launch before this one may have written: past L1
-  if (seq < 0) return;  // padding
+  if (seq < 0) return;                                                    // padding
   const int pos = a.row_pos ? __ldcg(a.row_pos + r) : slot;
-  const unsigned turn = pos < 0 ? 0u - (unsigned)pos : (unsigned)pos;
-  bool bad = seq >= a.n_seqs || slot < 0 || slot / a.page_size >= a.max_pages || (a.rotate && turn >= (unsigned)a.max_pos);
+  const unsigned turn = !a.rotate ? 0u : pos < 0 ? 0u - (unsigned)pos : (unsigned)pos;
+  const int nth = (int)((unsigned)slot / (unsigned)a.page_size), entry = slot - nth * a.page_size;
+  bool bad = seq >= a.n_seqs || slot < 0 || nth >= a.max_pages || turn >= (unsigned)a.max_pos;
   int page = 0;
   if (!bad) {
-    page = __ldcg(a.table + (long long)seq * a.max_pages + slot / a.page_size);
+    page = __ldcg(a.table + (long long)seq * a.max_pages + nth);
     bad = page < 0 || page >= a.n_pages;
   }
   if (bad) {
     if (u == 0) atomicOr(a.status, A3_DEV_BAD_POSITION);
     return;
   }
-  float f[16];
-  unpack8(x0, f);
-  unpack8(x1, f + 8);
-  if (what != 2 && a.rotate) {
-    const float sgn = pos < 0 ? -1.f : 1.f;
-    const float4* tr = reinterpret_cast<const float4*>(a.tab + (size_t)turn * (D / 2) + 8 * j);
+  // (cos, sin) of two frequencies each: 8j.. for pairs (i, i + D/2); 4j.. and 4j + D/4.. for pairs (2i, 2i+1)
+  float4 cs[4];
+  if (a.rotate) {
+    const float4* tr = reinterpret_cast<const float4*>(a.tab + (size_t)turn * (D / 2));
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float4 t = __ldg(tr + e);  // (cos, sin) of frequencies 8j + 2e and 8j + 2e + 1
-      const int p = LAYOUT == 0 ? 2 * e : 4 * e, step = LAYOUT == 0 ? 1 : 2, mate = LAYOUT == 0 ? 8 : 1;
-      const float a0 = f[p], b0 = f[p + mate], a1 = f[p + step], b1 = f[p + step + mate], s0 = sgn * t.y, s1 = sgn * t.w;
-      f[p] = a0 * t.x - b0 * s0;
-      f[p + mate] = a0 * s0 + b0 * t.x;
-      f[p + step] = a1 * t.z - b1 * s1;
-      f[p + step + mate] = a1 * s1 + b1 * t.z;
+      cs[e] = __ldg(tr + (LAYOUT == 0 ? 4 * j + e : 2 * j + e % 2 + e / 2 * (D / 8)));
+      if (pos < 0) cs[e].y = -cs[e].y, cs[e].w = -cs[e].w;
     }
   }
-  if (what == 0) {
-    bf16* dst = a.q_out + r * a.q_out_stride + head * D;
-    *reinterpret_cast<uint4*>(dst + lo) = pack8(f);
-    *reinterpret_cast<uint4*>(dst + hi) = pack8(f + 8);
-    return;
-  }
-  char* dst = (what == 1 ? a.k_pages : a.v_pages) + page * a.page_stride + ((long long)(slot % a.page_size) * a.kv_heads + head) * (D * (F8 ? 1 : 2));
-  if (F8) {
-    const float scale = (what == 1 ? a.k_scale : a.v_scale)[head];
-    *reinterpret_cast<uint2*>(dst + lo) = pack8_e4m3(f, scale);
-    *reinterpret_cast<uint2*>(dst + hi) = pack8_e4m3(f + 8, scale);
-  } else {
-    *reinterpret_cast<uint4*>(dst + 2 * lo) = pack8(f);
-    *reinterpret_cast<uint4*>(dst + 2 * hi) = pack8(f + 8);
+  const long long place = page * a.page_stride + (long long)entry * a.kv_heads * (D * (F8 ? 1 : 2));
+#pragma unroll
+  for (int i = 0; i < HEADS; ++i) {
+    const int h = h0 + i * stride;
+    if (h >= heads) break;
+    const bool is_v = h >= a.q_heads + a.kv_heads;
+    float f[16];
+    unpack8(x[i][0], f);
+    unpack8(x[i][1], f + 8);
+    if (!is_v && a.rotate) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int p = LAYOUT == 0 ? 2 * e : 4 * e, step = LAYOUT == 0 ? 1 : 2, mate = LAYOUT == 0 ? 8 : 1;
+        const float a0 = f[p], b0 = f[p + mate], a1 = f[p + step], b1 = f[p + step + mate];
+        f[p] = a0 * cs[e].x - b0 * cs[e].y;
+        f[p + mate] = a0 * cs[e].y + b0 * cs[e].x;
+        f[p + step] = a1 * cs[e].z - b1 * cs[e].w;
+        f[p + step + mate] = a1 * cs[e].w + b1 * cs[e].z;
+      }
+    }
+    if (h < a.q_heads) {
+      bf16* dst = a.q_out + r * a.q_out_stride + h * D + 8 * j;
+      *reinterpret_cast<uint4*>(dst) = pack8(f);
+      *reinterpret_cast<uint4*>(dst + D / 2) = pack8(f + 8);
+      continue;
+    }
+    const int kh = h - a.q_heads - (is_v ? a.kv_heads : 0);
+    char* dst = (is_v ? a.v_pages : a.k_pages) + place + (kh * D + 8 * j) * (F8 ? 1 : 2);
+    if (F8) {
+      const float by = 1.f / __ldg((is_v ? a.v_scale : a.k_scale) + kh);
+      *reinterpret_cast<uint2*>(dst) = pack8_e4m3(f, by);
+      *reinterpret_cast<uint2*>(dst + D / 2) = pack8_e4m3(f + 8, by);
+    } else {
+      *reinterpret_cast<uint4*>(dst) = pack8(f);
+      *reinterpret_cast<uint4*>(dst + D) = pack8(f + 8);
+    }
   }
 }
 
@@ -150,18 +172,21 @@ extern "C" int a3_paged_append(const a3_handle* h, const a3_paged_cache* cache, 
   a.q_out = (bf16*)q_out;
   a.M = M, a.q_heads = q_rows ? m.n_q_heads : 0, a.kv_heads = m.n_kv_heads;
   a.tab = h->rope_tab, a.max_pos = m.max_positions, a.rotate = rotate != 0, a.status = h->dev_status;
-  const unsigned long long units = (unsigned long long)M * (a.q_heads + 2 * a.kv_heads) * (m.head_dim / 16);
-  const unsigned long long blocks = (units + PA_THREADS - 1) / PA_THREADS;
-  if (blocks > 0x7fffffffull) return A3_EINVAL;
+  // one head for each thread as long as that fills the device, then four
+  const int all = a.q_heads + 2 * a.kv_heads, uph = m.head_dim / 16;
+  const bool many = (unsigned long long)M * all * uph > (unsigned long long)h->sm_count * PA_ONE;
+  const int heads = many ? PA_HEADS : 1;
+  const unsigned long long blocks = ((unsigned long long)M * cdiv(all, heads) * uph + PA_THREADS - 1) / PA_THREADS;
+  if (blocks * PA_THREADS > 0xffffffffull) return A3_ETOOLARGE;
   cudaStream_t st = (cudaStream_t)stream;
   ProfScope prof(h, A3_K_ROWS, st);
-  auto go = [&](auto kernel) { return launch_pdl(kernel, dim3((unsigned)blocks), dim3(PA_THREADS), 0, st, a); };
+  auto go = [&](auto one, auto four) { return launch_pdl(many ? four : one, dim3((unsigned)blocks), dim3(PA_THREADS), 0, st, a); };
   const bool f8 = cache->type == A3_CACHE_E4M3;
-  auto layout = [&](auto d) {
-    constexpr int DD = decltype(d)::value;
-    return m.rope_layout == 0 ? (f8 ? go(paged_append_kernel<DD, 0, true>) : go(paged_append_kernel<DD, 0, false>))
-                              : (f8 ? go(paged_append_kernel<DD, 1, true>) : go(paged_append_kernel<DD, 1, false>));
+  auto pick = [&](auto d, auto layout) {
+    constexpr int DD = decltype(d)::value, L = decltype(layout)::value;
+    return f8 ? go(paged_append_kernel<DD, L, true, 1>, paged_append_kernel<DD, L, true, PA_HEADS>) : go(paged_append_kernel<DD, L, false, 1>, paged_append_kernel<DD, L, false, PA_HEADS>);
   };
-  A3_CUDA(m.head_dim == 64 ? layout(std::integral_constant<int, 64>{}) : layout(std::integral_constant<int, 128>{}));
+  auto shape = [&](auto d) { return m.rope_layout == 0 ? pick(d, std::integral_constant<int, 0>{}) : pick(d, std::integral_constant<int, 1>{}); };
+  A3_CUDA(m.head_dim == 64 ? shape(std::integral_constant<int, 64>{}) : shape(std::integral_constant<int, 128>{}));
   return launched();
 }
