@@ -10,11 +10,9 @@
 
 namespace a3 {
 
-constexpr int PA_THREADS = 256;
-#ifndef PA_MIN
-#define PA_MIN 1
-#define PA_HEADS 4
-#endif
+constexpr int PA_THREADS = 128;
+constexpr int PA_MIN = 5;     // CTAs per SM: 96 registers hold the four heads and their cosines
+constexpr int PA_HEADS = 4;   // of a thread where rows are many
 constexpr int PA_ONE = 2048;  // units per SM up to which a thread moves one head
 
 struct AppendArgs {
@@ -50,83 +48,101 @@ paged_append_kernel(const AppendArgs a) {
   pdl_launch_dependents();
   constexpr int UPH = D / 16;  // units per head
   const int heads = a.q_heads + 2 * a.kv_heads, stride = (heads + HEADS - 1) / HEADS;  // of the thread's heads
-  const unsigned upr = (unsigned)stride * UPH;
-  const unsigned long long idx = (unsigned long long)blockIdx.x * PA_THREADS + threadIdx.x;
-  const int r = (int)(HEADS == 1 ? idx / upr : (unsigned)idx / upr);  // with several heads a launch has less than 2^32 threads
-  if (r >= a.M) return;
-  const int u = (int)(idx - (unsigned long long)r * upr), j = u % UPH, h0 = u / UPH;
-  uint4 x[HEADS][2];
+  const unsigned upr = (unsigned)stride * UPH, threads = gridDim.x * PA_THREADS;       // a thread's items are `threads` apart
+  const unsigned step_r = threads / upr, step_u = threads - step_r * upr;
+  unsigned r = (blockIdx.x * PA_THREADS + threadIdx.x) / upr, u = blockIdx.x * PA_THREADS + threadIdx.x - r * upr;
+  if (r >= (unsigned)a.M) return;
+  // Where a row goes is looked up while the row before it is moved: the chain from its slot over the page to the store is as long as two
+  // loads of the row itself.  A launch before this one may have written the indices: past L1.
+  int seq, slot, pos, page;
+  auto read_row = [&](unsigned row) {
+    seq = __ldcg(a.row_seq + row), slot = __ldcg(a.row_slot + row);
+    pos = a.row_pos ? __ldcg(a.row_pos + row) : slot;
+  };
+  unsigned turn, entry;
+  auto look_up = [&] {  // page: -2 for padding, -1 where the row leads nowhere
+    turn = !a.rotate ? 0u : pos < 0 ? 0u - (unsigned)pos : (unsigned)pos;
+    const unsigned nth = (unsigned)slot / (unsigned)a.page_size;
+    entry = (unsigned)slot - nth * a.page_size;
+    const bool good = seq >= 0 && seq < a.n_seqs && slot >= 0 && nth < (unsigned)a.max_pages && turn < (unsigned)a.max_pos;
+    page = good ? __ldcg(a.table + (long long)seq * a.max_pages + nth) : seq < 0 ? -2 : -1;
+  };
+  read_row(r);
+  look_up();
+  for (;;) {
+    const int j = u % UPH, h0 = u / UPH;
+    const bf16 *q = a.q + r * a.q_stride + 8 * j, *k = a.k + r * a.k_stride + 8 * j - a.q_heads * D, *v = a.v + r * a.v_stride + 8 * j - (a.q_heads + a.kv_heads) * D;
+    uint4 x[HEADS][2];
 #pragma unroll
-  for (int i = 0; i < HEADS; ++i) {
-    const int h = h0 + i * stride;
-    if (h < heads) {
-      const bf16* src = h < a.q_heads ? a.q + r * a.q_stride + h * D
-                        : h < a.q_heads + a.kv_heads ? a.k + r * a.k_stride + (h - a.q_heads) * D : a.v + r * a.v_stride + (h - a.q_heads - a.kv_heads) * D;
-      x[i][0] = __ldcs(reinterpret_cast<const uint4*>(src + 8 * j));
-      x[i][1] = __ldcs(reinterpret_cast<const uint4*>(src + 8 * j + D / 2));
-    }
-  }
-  const int seq = __ldcg(a.row_seq + r), slot = __ldcg(a.row_slot + r);  // what a launch before this one may have written: past L1
-  if (seq < 0) return;                                                    // padding
-  const int pos = a.row_pos ? __ldcg(a.row_pos + r) : slot;
-  const unsigned turn = !a.rotate ? 0u : pos < 0 ? 0u - (unsigned)pos : (unsigned)pos;
-  const int nth = (int)((unsigned)slot / (unsigned)a.page_size), entry = slot - nth * a.page_size;
-  bool bad = seq >= a.n_seqs || slot < 0 || nth >= a.max_pages || turn >= (unsigned)a.max_pos;
-  int page = 0;
-  if (!bad) {
-    page = __ldcg(a.table + (long long)seq * a.max_pages + nth);
-    bad = page < 0 || page >= a.n_pages;
-  }
-  if (bad) {
-    if (u == 0) atomicOr(a.status, A3_DEV_BAD_POSITION);
-    return;
-  }
-  // (cos, sin) of two frequencies each: 8j.. for pairs (i, i + D/2); 4j.. and 4j + D/4.. for pairs (2i, 2i+1)
-  float4 cs[4];
-  if (a.rotate) {
-    const float4* tr = reinterpret_cast<const float4*>(a.tab + (size_t)turn * (D / 2));
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      cs[e] = __ldg(tr + (LAYOUT == 0 ? 4 * j + e : 2 * j + e % 2 + e / 2 * (D / 8)));
-      if (pos < 0) cs[e].y = -cs[e].y, cs[e].w = -cs[e].w;
-    }
-  }
-  const long long place = page * a.page_stride + (long long)entry * a.kv_heads * (D * (F8 ? 1 : 2));
-#pragma unroll
-  for (int i = 0; i < HEADS; ++i) {
-    const int h = h0 + i * stride;
-    if (h >= heads) break;
-    const bool is_v = h >= a.q_heads + a.kv_heads;
-    float f[16];
-    unpack8(x[i][0], f);
-    unpack8(x[i][1], f + 8);
-    if (!is_v && a.rotate) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int p = LAYOUT == 0 ? 2 * e : 4 * e, step = LAYOUT == 0 ? 1 : 2, mate = LAYOUT == 0 ? 8 : 1;
-        const float a0 = f[p], b0 = f[p + mate], a1 = f[p + step], b1 = f[p + step + mate];
-        f[p] = a0 * cs[e].x - b0 * cs[e].y;
-        f[p + mate] = a0 * cs[e].y + b0 * cs[e].x;
-        f[p + step] = a1 * cs[e].z - b1 * cs[e].w;
-        f[p + step + mate] = a1 * cs[e].w + b1 * cs[e].z;
+    for (int i = 0; i < HEADS; ++i) {
+      const int h = h0 + i * stride;
+      if (h < heads) {
+        const bf16* src = (h < a.q_heads ? q : h < a.q_heads + a.kv_heads ? k : v) + h * D;
+        x[i][0] = __ldcs(reinterpret_cast<const uint4*>(src));
+        x[i][1] = __ldcs(reinterpret_cast<const uint4*>(src + D / 2));
       }
     }
-    if (h < a.q_heads) {
-      bf16* dst = a.q_out + r * a.q_out_stride + h * D + 8 * j;
-      *reinterpret_cast<uint4*>(dst) = pack8(f);
-      *reinterpret_cast<uint4*>(dst + D / 2) = pack8(f + 8);
-      continue;
+    const bool turned = a.rotate && pos < 0, live = page != -2;
+    const int this_page = page, this_entry = entry;
+    const unsigned this_r = r, this_u = u;
+    // (cos, sin) of two frequencies each: 8j.. for pairs (i, i + D/2); 4j.. and 4j + D/4.. for pairs (2i, 2i+1)
+    float4 cs[4];
+    if (a.rotate && turn < (unsigned)a.max_pos) {
+      const float4* tr = reinterpret_cast<const float4*>(a.tab + (size_t)turn * (D / 2));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) cs[e] = __ldg(tr + (LAYOUT == 0 ? 4 * j + e : 2 * j + e % 2 + e / 2 * (D / 8)));
     }
-    const int kh = h - a.q_heads - (is_v ? a.kv_heads : 0);
-    char* dst = (is_v ? a.v_pages : a.k_pages) + place + (kh * D + 8 * j) * (F8 ? 1 : 2);
-    if (F8) {
-      const float by = 1.f / __ldg((is_v ? a.v_scale : a.k_scale) + kh);
-      *reinterpret_cast<uint2*>(dst) = pack8_e4m3(f, by);
-      *reinterpret_cast<uint2*>(dst + D / 2) = pack8_e4m3(f + 8, by);
-    } else {
-      *reinterpret_cast<uint4*>(dst) = pack8(f);
-      *reinterpret_cast<uint4*>(dst + D) = pack8(f + 8);
+    r += step_r;
+    if ((u += step_u) >= upr) u -= upr, ++r;
+    const bool more = r < (unsigned)a.M;
+    if (more) read_row(r);
+    if (live && (this_page < 0 || this_page >= a.n_pages)) {
+      if (this_u == 0) atomicOr(a.status, A3_DEV_BAD_POSITION);
+    } else if (live) {
+      const long long place = this_page * a.page_stride + (long long)this_entry * a.kv_heads * (D * (F8 ? 1 : 2)) + 8 * j * (F8 ? 1 : 2);
+      if (turned) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) cs[e].y = -cs[e].y, cs[e].w = -cs[e].w;
+      }
+#pragma unroll
+      for (int i = 0; i < HEADS; ++i) {
+        const int h = h0 + i * stride;
+        if (h >= heads) break;
+        const bool is_v = h >= a.q_heads + a.kv_heads;
+        float f[16];
+        unpack8(x[i][0], f);
+        unpack8(x[i][1], f + 8);
+        if (!is_v && a.rotate) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int p = LAYOUT == 0 ? 2 * e : 4 * e, step = LAYOUT == 0 ? 1 : 2, mate = LAYOUT == 0 ? 8 : 1;
+            const float a0 = f[p], b0 = f[p + mate], a1 = f[p + step], b1 = f[p + step + mate];
+            f[p] = a0 * cs[e].x - b0 * cs[e].y;
+            f[p + mate] = a0 * cs[e].y + b0 * cs[e].x;
+            f[p + step] = a1 * cs[e].z - b1 * cs[e].w;
+            f[p + step + mate] = a1 * cs[e].w + b1 * cs[e].z;
+          }
+        }
+        if (h < a.q_heads) {
+          bf16* dst = a.q_out + this_r * a.q_out_stride + h * D + 8 * j;
+          *reinterpret_cast<uint4*>(dst) = pack8(f);
+          *reinterpret_cast<uint4*>(dst + D / 2) = pack8(f + 8);
+          continue;
+        }
+        const int kh = h - a.q_heads - (is_v ? a.kv_heads : 0);
+        char* dst = (is_v ? a.v_pages : a.k_pages) + place + kh * (D * (F8 ? 1 : 2));
+        if (F8) {
+          const float by = __frcp_rn(__ldg((is_v ? a.v_scale : a.k_scale) + kh));
+          *reinterpret_cast<uint2*>(dst) = pack8_e4m3(f, by);
+          *reinterpret_cast<uint2*>(dst + D / 2) = pack8_e4m3(f + 8, by);
+        } else {
+          *reinterpret_cast<uint4*>(dst) = pack8(f);
+          *reinterpret_cast<uint4*>(dst + D) = pack8(f + 8);
+        }
+      }
     }
+    if (!more) return;
+    look_up();
   }
 }
 
@@ -176,11 +192,11 @@ extern "C" int a3_paged_append(const a3_handle* h, const a3_paged_cache* cache, 
   const int all = a.q_heads + 2 * a.kv_heads, uph = m.head_dim / 16;
   const bool many = (unsigned long long)M * all * uph > (unsigned long long)h->sm_count * PA_ONE;
   const int heads = many ? PA_HEADS : 1;
-  const unsigned long long blocks = ((unsigned long long)M * cdiv(all, heads) * uph + PA_THREADS - 1) / PA_THREADS;
-  if (blocks * PA_THREADS > 0xffffffffull) return A3_ETOOLARGE;
+  const unsigned long long need = ((unsigned long long)M * cdiv(all, heads) * uph + PA_THREADS - 1) / PA_THREADS;
+  const unsigned blocks = (unsigned)(need < (unsigned long long)h->sm_count * PA_MIN ? need : (unsigned long long)h->sm_count * PA_MIN);
   cudaStream_t st = (cudaStream_t)stream;
   ProfScope prof(h, A3_K_ROWS, st);
-  auto go = [&](auto one, auto four) { return launch_pdl(many ? four : one, dim3((unsigned)blocks), dim3(PA_THREADS), 0, st, a); };
+  auto go = [&](auto one, auto four) { return launch_pdl(many ? four : one, dim3(blocks), dim3(PA_THREADS), 0, st, a); };
   const bool f8 = cache->type == A3_CACHE_E4M3;
   auto pick = [&](auto d, auto layout) {
     constexpr int DD = decltype(d)::value, L = decltype(layout)::value;
