@@ -8,8 +8,8 @@
 // running (M, s, w) of its own elements.  s is carried without the 1 of one largest element and ends in log1p: where one token
 // has nearly all of the probability, what it lacks of 1 and the entropy come from the other tokens alone.
 //
-// The alternatives come from the same pass: the n-th largest of the threads' maxima is a bound that at least n elements reach, and only
-// the threads whose own maximum reaches it - little more than n of 512 - are gone through again (from L2), a warp together on one
+// The alternatives come from the same pass: the n-th largest of the threads' maxima (of the four largest of each warp) is a bound that at least n elements reach, and only
+// the threads whose own maximum reaches it - little more than n of 256 - are gone through again (from L2), a warp together on one
 // thread's elements.  What reaches the bound, usually 1-2 n elements, is ranked by counting.
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
@@ -18,7 +18,13 @@
 
 namespace a3 {
 
-constexpr int LP_THREADS = 512, LP_WARPS = LP_THREADS / 32, LP_U = 4, LP_CAP = 1024, LP_TOP = A3_LOGPROBS_MAX_TOP;
+constexpr int LP_THREADS = 256, LP_WARPS = LP_THREADS / 32, LP_U = 4, LP_CAP = 2048, LP_TOP = A3_LOGPROBS_MAX_TOP;
+constexpr int LP_KEPT = 32 / LP_WARPS;  // largest maxima of a warp's lanes that the bound is taken from: 32 in all
+static_assert(LP_KEPT * LP_WARPS >= LP_TOP, "the bound is the n-th largest of them");
+constexpr int LP_MIN = 4;     // CTAs per SM
+constexpr int LP_STAGES = 3;  // batches of LP_U vectors for each thread
+constexpr int LP_RING = LP_STAGES * LP_U * LP_THREADS * 16;
+static_assert(LP_CAP * 8 <= LP_RING, "candidates lie in the ring");
 constexpr float LOG2E = 1.44269504088896341f;
 constexpr float LP_FAR = -200.f;  // exp of it is 0 in fp32, and unlike that of -inf or of the lowest value its product with that 0 is 0 too
 
@@ -34,28 +40,102 @@ struct LogprobArgs {
   uint32_t* status;
 };
 
+// Pairs of fp32 in one 64-bit register: additions and products of two at once.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pack_f2(float x, float y) {
+  f32x2 z;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(z) : "f"(x), "f"(y));
+  return z;
+}
+__device__ __forceinline__ float2 unpack_f2(f32x2 z) {
+  float2 v;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(z));
+  return v;
+}
+__device__ __forceinline__ f32x2 add_f2(f32x2 a, f32x2 b) {
+  f32x2 z;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(z) : "l"(a), "l"(b));
+  return z;
+}
+__device__ __forceinline__ f32x2 mul_f2(f32x2 a, f32x2 b) {
+  f32x2 z;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(z) : "l"(a), "l"(b));
+  return z;
+}
+__device__ __forceinline__ f32x2 fma_f2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 z;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(z) : "l"(a), "l"(b), "l"(c));
+  return z;
+}
+
+// VE values of a 16-byte vector, W words of it that hold them: the largest number of vectors, word by word (`max_of`, then `largest`), and the
+// values of a word as pairs, those of -inf as the type's lowest number (NaN stays).
 template <typename T>
 struct Logit;
 template <>
 struct Logit<float> {
   static constexpr int VE = 4;
+  static constexpr float LOWEST = -3.40282347e38f;
+  __device__ static uint4 max_of(uint4 a, uint4 b) { return make_uint4(two(a.x, b.x), two(a.y, b.y), two(a.z, b.z), two(a.w, b.w)); }
+  __device__ static uint32_t two(uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }
+  __device__ static float largest(uint4 v) { return __uint_as_float(two(two(v.x, v.y), two(v.z, v.w))); }
+  __device__ static void pairs(const uint4& v, f32x2* p) { p[0] = pack_f2(finite(v.x), finite(v.y)), p[1] = pack_f2(finite(v.z), finite(v.w)); }
+  __device__ static float finite(uint32_t x) {
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(__uint_as_float(x)), "f"(LOWEST));
+    return y;
+  }
   __device__ static void unpack(const uint4& v, float* f) { f[0] = __uint_as_float(v.x), f[1] = __uint_as_float(v.y), f[2] = __uint_as_float(v.z), f[3] = __uint_as_float(v.w); }
   __device__ static float one(const float* p) { return *p; }
 };
 template <>
 struct Logit<bf16> {
   static constexpr int VE = 8;
+  static constexpr float LOWEST = -3.38953139e38f;
+  __device__ static uint4 max_of(uint4 a, uint4 b) { return make_uint4(two(a.x, b.x), two(a.y, b.y), two(a.z, b.z), two(a.w, b.w)); }
+  __device__ static uint32_t two(uint32_t a, uint32_t b) {
+    uint32_t y;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b));
+    return y;
+  }
+  __device__ static float largest(uint4 v) {
+    const uint32_t x = two(two(v.x, v.y), two(v.z, v.w));
+    return fmaxf(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
+  }
+  __device__ static f32x2 pair(uint32_t x) {
+    asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(x) : "r"(0xff7fff7fu));
+    return pack_f2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
+  }
+  __device__ static void pairs(const uint4& v, f32x2* p) { p[0] = pair(v.x), p[1] = pair(v.y), p[2] = pair(v.z), p[3] = pair(v.w); }
   __device__ static void unpack(const uint4& v, float* f) { unpack8(v, f); }
   __device__ static float one(const bf16* p) { return __bfloat162float(*p); }
 };
 template <>
 struct Logit<__half> {
   static constexpr int VE = 8;
+  static constexpr float LOWEST = -65504.f;
+  __device__ static uint4 max_of(uint4 a, uint4 b) { return make_uint4(two(a.x, b.x), two(a.y, b.y), two(a.z, b.z), two(a.w, b.w)); }
+  __device__ static uint32_t two(uint32_t a, uint32_t b) {
+    uint32_t y;
+    asm("max.f16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b));
+    return y;
+  }
+  __device__ static float2 floats(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2*>(&x)); }
+  __device__ static float largest(uint4 v) {
+    const float2 t = floats(two(two(v.x, v.y), two(v.z, v.w)));
+    return fmaxf(t.x, t.y);
+  }
+  __device__ static f32x2 pair(uint32_t x) {
+    asm("max.NaN.f16x2 %0, %0, %1;" : "+r"(x) : "r"(0xfbfffbffu));
+    const float2 t = floats(x);
+    return pack_f2(t.x, t.y);
+  }
+  __device__ static void pairs(const uint4& v, f32x2* p) { p[0] = pair(v.x), p[1] = pair(v.y), p[2] = pair(v.z), p[3] = pair(v.w); }
   __device__ static void unpack(const uint4& v, float* f) {
-    const __half2* p = reinterpret_cast<const __half2*>(&v);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float2 t = __half22float2(p[i]);
+      const float2 t = floats(w[i]);
       f[2 * i] = t.x, f[2 * i + 1] = t.y;
     }
   }
@@ -93,13 +173,16 @@ __device__ __forceinline__ float warp_sum(float x) {
 }
 
 template <typename T>
-__global__ void __launch_bounds__(LP_THREADS, 2)
+__global__ void __launch_bounds__(LP_THREADS, LP_MIN)
 logprobs_kernel(const LogprobArgs a) {
   namespace cg = cooperative_groups;
   constexpr int VE = Logit<T>::VE;
   __shared__ LpStats s_stats;
   __shared__ float s_red[3][LP_WARPS];
-  __shared__ unsigned long long s_cand[LP_CAP], s_top[LP_TOP], s_best[LP_WARPS];
+  extern __shared__ __align__(16) uint4 ring[];
+  unsigned long long* s_cand = reinterpret_cast<unsigned long long*>(ring);  // once the ring is done with
+  __shared__ unsigned long long s_top[LP_TOP], s_best[LP_WARPS];
+  __shared__ uint32_t s_kept[32];
   __shared__ int s_count, s_holder;
   pdl_wait();
   pdl_launch_dependents();
@@ -118,18 +201,21 @@ logprobs_kernel(const LogprobArgs a) {
   if (rank == parts - 1 && tid >= 32 && tid - 32 < a.vocab - tail0) single = tail0 + tid - 32;
 
   float m = -INFINITY, s = 0.f, w = 0.f;
-  auto take = [&](const float* f, int n) {
-    float most = f[0];
-#pragma unroll
-    for (int i = 1; i < n; ++i) most = fmaxf(most, f[i]);  // of the numbers
+  f32x2 s2 = 0, w2 = 0;  // the vectors' share of s and w, two sums each
+  auto raise = [&](float most) {
     if (most > m) {
       if (m > -INFINITY) {
         const float d = fmaxf(m - most, LP_FAR), g = lp_ex2(d * LOG2E);
         w = g * (w + s * d);
         s *= g;
+        const f32x2 gg = pack_f2(g, g);
+        w2 = mul_f2(gg, fma_f2(s2, pack_f2(d, d), w2));
+        s2 = mul_f2(gg, s2);
       }
       m = most;
     }
+  };
+  auto add = [&](const float* f, int n) {  // any values
     if (m > -INFINITY) {
 #pragma unroll
       for (int i = 0; i < n; ++i) {
@@ -143,24 +229,75 @@ logprobs_kernel(const LogprobArgs a) {
         if (f[i] != f[i]) s = NAN;
     }
   };
-  for (int v = v0 + tid; v < v1; v += LP_THREADS * LP_U) {
+  // Vectors at hand at once: one look at whether the maximum rises.  With a maximum in the ordinary range -inf may stand as the type's
+  // lowest number: its exponential is 0 and the product of the two is.
+  auto take = [&](const uint4* at, int n) {  // at, at + LP_THREADS, ...: n of them
     uint4 raw[LP_U];
-    float f[LP_U * VE];
 #pragma unroll
-    for (int u = 0; u < LP_U; ++u)
-      if (v + u * LP_THREADS < v1) raw[u] = __ldg(xv + v + u * LP_THREADS);
+    for (int u = 0; u < LP_U; ++u) raw[u] = at[u * LP_THREADS];  // behind the n-th: not used
+    uint4 top = raw[0];
 #pragma unroll
-    for (int u = 0; u < LP_U; ++u) {
-      if (v + u * LP_THREADS < v1) {
-        Logit<T>::unpack(raw[u], f);
-        take(f, VE);
+    for (int u = 1; u < LP_U; ++u)
+      if (u < n) top = Logit<T>::max_of(top, raw[u]);
+    raise(Logit<T>::largest(top));
+    if (m > Logit<T>::LOWEST && m < 1e30f) {
+      const f32x2 ref = pack_f2(-m, -m), log2e = pack_f2(LOG2E, LOG2E);
+#pragma unroll
+      for (int u = 0; u < LP_U; ++u) {
+        if (u < n) {
+          f32x2 p[VE / 2];
+          Logit<T>::pairs(raw[u], p);
+#pragma unroll
+          for (int i = 0; i < VE / 2; ++i) {
+            const f32x2 d = add_f2(p[i], ref);
+            const float2 t = unpack_f2(mul_f2(d, log2e));
+            const f32x2 e = pack_f2(lp_ex2(t.x), lp_ex2(t.y));
+            s2 = add_f2(s2, e);
+            w2 = fma_f2(e, d, w2);
+          }
+        }
+      }
+    } else {
+#pragma unroll 1
+      for (int u = 0; u < n; ++u) {
+        float f[VE];
+        Logit<T>::unpack(at[u * LP_THREADS], f);
+        add(f, VE);
       }
     }
+  };
+  {
+    // Each thread's vectors come through a ring of its own in shared memory, LP_STAGES - 1 batches under way while one is computed: what the
+    // registers of all threads hold is too little to cover the way from HBM.
+    const uint32_t mine_u = smem_u32(ring + tid);
+    constexpr int BATCH = LP_THREADS * LP_U;
+    auto fetch = [&](int b) {
+      const int v = v0 + tid + b * BATCH;
+#pragma unroll
+      for (int u = 0; u < LP_U; ++u)
+        if (v + u * LP_THREADS < v1) cp_async16(mine_u + (b % LP_STAGES * BATCH + u * LP_THREADS) * 16, xv + v + u * LP_THREADS, true);
+      cp_async_commit();
+    };
+#pragma unroll 1
+    for (int b = 0; b < LP_STAGES - 1; ++b) fetch(b);
+    int b = 0;
+    for (int v = v0 + tid; v < v1; v += BATCH, ++b) {
+      fetch(b + LP_STAGES - 1);
+      cp_async_wait<LP_STAGES - 1>();
+      take(ring + tid + b % LP_STAGES * BATCH, min(LP_U, (v1 - v + LP_THREADS - 1) / LP_THREADS));
+    }
+  }
+  {
+    const float2 ss = unpack_f2(s2), ww = unpack_f2(w2);
+    s += ss.x + ss.y;
+    w += ww.x + ww.y;
+    s2 = w2 = 0;
   }
   const uint32_t mine = ordered(m);  // of the vectors alone; LP_NONE: nothing above -inf
   if (single >= 0) {
     const float f = Logit<T>::one(x + single);
-    take(&f, 1);
+    raise(f);
+    add(&f, 1);
   }
 
   // ---- the CTA's statistics
@@ -169,6 +306,15 @@ logprobs_kernel(const LogprobArgs a) {
 #pragma unroll
   for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
   if (lane == 0) s_red[0][warp] = most;
+  if (a.n_top > 0) {
+    uint32_t o = mine;
+#pragma unroll
+    for (int k = 0; k < LP_KEPT; ++k) {
+      const uint32_t best = __reduce_max_sync(0xffffffffu, o);
+      if (lane == 0) s_kept[warp * LP_KEPT + k] = best;
+      if (lane == __ffs(__ballot_sync(0xffffffffu, o == best)) - 1) o = 0;
+    }
+  }
   __syncthreads();
   most = s_red[0][0];
 #pragma unroll
@@ -192,12 +338,13 @@ logprobs_kernel(const LogprobArgs a) {
   // ---- the CTA's best elements above -inf
   if (a.n_top > 0) {
     const int n = a.n_top;
-    // a bound that n threads' maxima reach (its upper 16 bits: a lower one does as well)
+    // a bound that n threads' maxima reach: the n-th largest of those kept (its upper 16 bits: a lower one does as well)
+    const uint32_t kept = s_kept[lane];
     uint32_t bound = 0;
 #pragma unroll
     for (int bit = 31; bit >= 16; --bit) {
       const uint32_t c = bound | 1u << bit;
-      if (__syncthreads_count(mine >= c) >= n) bound = c;
+      if (__popc(__ballot_sync(0xffffffffu, kept >= c)) >= n) bound = c;
     }
     if (bound <= LP_NONE) bound = LP_NONE + 1;
     auto offer = [&](float f, int id) {
@@ -350,11 +497,13 @@ logprobs_kernel(const LogprobArgs a) {
 
 template <typename T>
 static int logprobs_launch(const a3_handle* h, const LogprobArgs& a, cudaStream_t st) {
-  // CTAs per row: as many as the device holds at two per SM, and no fewer than 2 048 elements for each
+  // CTAs per row: as many as the device holds, and no fewer than 2 048 elements for each
   int parts = 1;
-  while (parts < 8 && (long long)a.M * parts * 2 <= 2 * h->sm_count && a.vocab / (2 * parts) >= 2048) parts *= 2;
+  while (parts < 8 && (long long)a.M * parts * 2 <= LP_MIN * h->sm_count && a.vocab / (2 * parts) >= 2048) parts *= 2;
   if ((long long)a.M * parts > 0x7fffffffll) return A3_EINVAL;
-  A3_CUDA(launch_pdl_cluster(parts, logprobs_kernel<T>, dim3((unsigned)(a.M * parts)), dim3(LP_THREADS), 0, st, a));
+  static SmemAttrOnce once;
+  A3_TRY(smem_attr_once(once, h->device, logprobs_kernel<T>, LP_RING));
+  A3_CUDA(launch_pdl_cluster(parts, logprobs_kernel<T>, dim3((unsigned)(a.M * parts)), dim3(LP_THREADS), LP_RING, st, a));
   return launched();
 }
 
