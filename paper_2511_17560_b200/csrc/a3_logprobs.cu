@@ -11,20 +11,18 @@
 // The alternatives come from the same pass: the n-th largest of the threads' maxima (of the four largest of each warp) is a bound that at least n elements reach, and only
 // the threads whose own maximum reaches it - little more than n of 256 - are gone through again (from L2), a warp together on one
 // thread's elements.  What reaches the bound, usually 1-2 n elements, is ranked by counting.
-#include <cooperative_groups.h>
 #include <cuda_fp16.h>
 
 #include "a3_internal.cuh"
 
 namespace a3 {
 
-constexpr int LP_THREADS = 256, LP_WARPS = LP_THREADS / 32, LP_U = 4, LP_CAP = 2048, LP_TOP = A3_LOGPROBS_MAX_TOP;
+constexpr int LP_THREADS = 256, LP_WARPS = LP_THREADS / 32, LP_U = 4, LP_CAP = 512, LP_PARTS = 8, LP_TOP = A3_LOGPROBS_MAX_TOP;
 constexpr int LP_KEPT = 32 / LP_WARPS;  // largest maxima of a warp's lanes that the bound is taken from: 32 in all
 static_assert(LP_KEPT * LP_WARPS >= LP_TOP, "the bound is the n-th largest of them");
 constexpr int LP_MIN = 4;     // CTAs per SM
 constexpr int LP_STAGES = 3;  // batches of LP_U vectors for each thread
 constexpr int LP_RING = LP_STAGES * LP_U * LP_THREADS * 16;
-static_assert(LP_CAP * 8 <= LP_RING, "candidates lie in the ring");
 constexpr float LOG2E = 1.44269504088896341f;
 constexpr float LP_FAR = -200.f;  // exp of it is 0 in fp32, and unlike that of -inf or of the lowest value its product with that 0 is 0 too
 
@@ -166,6 +164,32 @@ __device__ __forceinline__ int key_id(unsigned long long k) { return (int)(0xfff
 struct LpStats {
   float m, s, w;  // s without the 1 of one largest element
 };
+// Clusters: this CTA's place, the barrier in halves (all threads arrive; what was written before is seen behind the wait), and the place of
+// a variable of this CTA in the first one of its cluster.
+__device__ __forceinline__ uint32_t cluster_size() {
+  uint32_t x;
+  asm("mov.u32 %0, %cluster_nctaid.x;" : "=r"(x));
+  return x;
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t x;
+  asm("mov.u32 %0, %cluster_ctarank;" : "=r"(x));
+  return x;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+template <typename V>
+__device__ __forceinline__ V* in_first(V* p, int parts) {
+  if (parts == 1) return p;
+  V* q;
+  asm("mapa.u64 %0, %1, %2;" : "=l"(q) : "l"(p), "r"(0));
+  return q;
+}
+__device__ __forceinline__ float warp_max(float x) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+  return x;
+}
 __device__ __forceinline__ float warp_sum(float x) {
 #pragma unroll
   for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
@@ -175,19 +199,19 @@ __device__ __forceinline__ float warp_sum(float x) {
 template <typename T>
 __global__ void __launch_bounds__(LP_THREADS, LP_MIN)
 logprobs_kernel(const LogprobArgs a) {
-  namespace cg = cooperative_groups;
   constexpr int VE = Logit<T>::VE;
-  __shared__ LpStats s_stats;
-  __shared__ float s_red[3][LP_WARPS];
   extern __shared__ __align__(16) uint4 ring[];
-  unsigned long long* s_cand = reinterpret_cast<unsigned long long*>(ring);  // once the ring is done with
-  __shared__ unsigned long long s_top[LP_TOP], s_best[LP_WARPS];
+  __shared__ float s_red[3][LP_WARPS];
   __shared__ uint32_t s_kept[32];
-  __shared__ int s_count, s_holder;
+  __shared__ unsigned long long s_cand[LP_CAP], s_best[LP_WARPS];
+  __shared__ int s_count;
+  // of the row, in its first CTA: every CTA's statistics and best elements (in descending order, 0 where there are fewer), and the row's
+  __shared__ LpStats s_stats[LP_PARTS];
+  __shared__ unsigned long long s_lists[LP_PARTS][LP_TOP], s_top[LP_TOP];
+  const int parts = (int)cluster_size(), rank = (int)cluster_rank();
+  if (parts > 1) cluster_arrive();  // waited for before the first access to another CTA's memory: it has to be there
   pdl_wait();
   pdl_launch_dependents();
-  cg::cluster_group cluster = cg::this_cluster();
-  const int parts = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int row = blockIdx.x / parts, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const T* x = reinterpret_cast<const T*>(a.logits) + row * a.row_stride;
   // 16-byte vectors from the first boundary on, the few elements before and behind them one by one
@@ -199,6 +223,10 @@ logprobs_kernel(const LogprobArgs a) {
   int single = -1;
   if (rank == 0 && tid < head) single = tid;
   if (rank == parts - 1 && tid >= 32 && tid - 32 < a.vocab - tail0) single = tail0 + tid - 32;
+
+  // the given token's logit, on its way from here on
+  const int target = rank == 0 && a.targets ? __ldcg(a.targets + row) : -1;
+  const float target_logit = tid == 0 && target >= 0 && target < a.vocab ? Logit<T>::one(x + target) : 0.f;
 
   float m = -INFINITY, s = 0.f, w = 0.f;
   f32x2 s2 = 0, w2 = 0;  // the vectors' share of s and w, two sums each
@@ -300,82 +328,107 @@ logprobs_kernel(const LogprobArgs a) {
     add(&f, 1);
   }
 
-  // ---- the CTA's statistics
-  if (tid == 0) s_count = 0, s_holder = LP_THREADS;
-  float most = m;
+  // ---- the CTA's statistics; its largest elements' bound
+  if (tid == 0) s_count = 0;
+  const int n = a.n_top;
+  {
+    const float top = warp_max(m);
+    if (lane == 0) s_red[0][warp] = top;
+    if (n > 0) {
+      uint32_t o = mine;
 #pragma unroll
-  for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-  if (lane == 0) s_red[0][warp] = most;
-  if (a.n_top > 0) {
-    uint32_t o = mine;
-#pragma unroll
-    for (int k = 0; k < LP_KEPT; ++k) {
-      const uint32_t best = __reduce_max_sync(0xffffffffu, o);
-      if (lane == 0) s_kept[warp * LP_KEPT + k] = best;
-      if (lane == __ffs(__ballot_sync(0xffffffffu, o == best)) - 1) o = 0;
+      for (int k = 0; k < LP_KEPT; ++k) {
+        const uint32_t best = __reduce_max_sync(0xffffffffu, o);
+        if (lane == 0) s_kept[warp * LP_KEPT + k] = best;
+        if (lane == __ffs(__ballot_sync(0xffffffffu, o == best)) - 1) o = 0;
+      }
     }
   }
   __syncthreads();
-  most = s_red[0][0];
+  float most = s_red[0][0];
+  int holder = 0;  // the warp of one largest element, which s leaves out
 #pragma unroll
-  for (int i = 1; i < LP_WARPS; ++i) most = fmaxf(most, s_red[0][i]);
-  if (m == most) atomicMin(&s_holder, tid);
-  __syncthreads();
+  for (int i = 1; i < LP_WARPS; ++i)
+    if (s_red[0][i] > most) most = s_red[0][i], holder = i;
   {
+    const uint32_t these = __ballot_sync(0xffffffffu, m == most);
     const float d = fmaxf(m - most, LP_FAR), g = m > -INFINITY ? lp_ex2(d * LOG2E) : 0.f;
-    float ps = g * (tid == s_holder ? s - 1.f : s), pw = m > -INFINITY ? g * (w + s * d) : 0.f;
-    ps = warp_sum(ps);
-    pw = warp_sum(pw);
+    const float ps = warp_sum(g * (warp == holder && lane == __ffs(these) - 1 ? s - 1.f : s));
+    const float pw = warp_sum(m > -INFINITY ? g * (w + s * d) : 0.f);
     if (lane == 0) s_red[1][warp] = ps, s_red[2][warp] = pw;
-  }
-  __syncthreads();
-  if (tid == 0) {
-    float ps = 0.f, pw = 0.f;
-    for (int i = 0; i < LP_WARPS; ++i) ps += s_red[1][i], pw += s_red[2][i];
-    s_stats = LpStats{most, ps, pw};
   }
 
   // ---- the CTA's best elements above -inf
-  if (a.n_top > 0) {
-    const int n = a.n_top;
-    // a bound that n threads' maxima reach: the n-th largest of those kept (its upper 16 bits: a lower one does as well)
-    const uint32_t kept = s_kept[lane];
-    uint32_t bound = 0;
+  uint32_t bound = 0;
+  // one thread's elements, a warp together: `use(value, id)` for each
+  auto again = [&](int t, auto use) {
+    for (int v = v0 + t + lane * LP_THREADS; v < v1; v += 32 * LP_THREADS) {
+      float f[VE];
+      Logit<T>::unpack(__ldg(xv + v), f);
 #pragma unroll
-    for (int bit = 31; bit >= 16; --bit) {
-      const uint32_t c = bound | 1u << bit;
-      if (__popc(__ballot_sync(0xffffffffu, kept >= c)) >= n) bound = c;
+      for (int e = 0; e < VE; ++e) use(f[e], head + v * VE + e);
+    }
+  };
+  if (n > 0) {
+    // A bound that n threads' maxima reach: the n-th largest of those kept, or of all where not every thread has a vector (the upper 16 bits:
+    // a lower bound does as well).
+    if (v1 - v0 >= LP_THREADS) {
+      const uint32_t kept = s_kept[lane];
+#pragma unroll 1
+      for (int bit = 31; bit >= 16; --bit) {
+        const uint32_t c = bound | 1u << bit;
+        if (__popc(__ballot_sync(0xffffffffu, kept >= c)) >= n) bound = c;
+      }
+    } else {
+#pragma unroll 1
+      for (int bit = 31; bit >= 16; --bit) {
+        const uint32_t c = bound | 1u << bit;
+        if (__syncthreads_count(mine >= c) >= n) bound = c;
+      }
     }
     if (bound <= LP_NONE) bound = LP_NONE + 1;
+    const float least = unordered(bound);
     auto offer = [&](float f, int id) {
-      const uint32_t o = ordered(f);
-      if (o >= bound) {
+      if (f >= least) {
         const int at = atomicAdd(&s_count, 1);
-        if (at < LP_CAP) s_cand[at] = lp_key(o, id);
+        if (at < LP_CAP) s_cand[at] = lp_key(ordered(f), id);
       }
     };
-    // one thread's elements, a warp together: `use(value, id)` for each
-    auto again = [&](int t, auto use) {
-      for (int v = v0 + t + lane * LP_THREADS; v < v1; v += 32 * LP_THREADS) {
-        float f[VE];
-        Logit<T>::unpack(__ldg(xv + v), f);
+    if (v1 - v0 <= LP_STAGES * LP_U * LP_THREADS) {  // all of the CTA's vectors are still in the ring, each thread's at its hand
+      if (mine >= bound) {
+#pragma unroll 1
+        for (int v = v0 + tid, i = tid; v < v1; v += LP_THREADS, i += LP_THREADS) {
+          const uint4 raw = ring[i];
+          if (!(Logit<T>::largest(raw) >= least)) continue;
+          float f[VE];
+          Logit<T>::unpack(raw, f);
 #pragma unroll
-        for (int e = 0; e < VE; ++e) use(f[e], head + v * VE + e);
+          for (int e = 0; e < VE; ++e) offer(f[e], head + v * VE + e);
+        }
       }
-    };
-    for (uint32_t left = __ballot_sync(0xffffffffu, mine >= bound); left; left &= left - 1) again(warp * 32 + __ffs(left) - 1, offer);
+    } else {
+      for (uint32_t left = __ballot_sync(0xffffffffu, mine >= bound); left; left &= left - 1) again(warp * 32 + __ffs(left) - 1, offer);
+    }
     if (single >= 0) offer(Logit<T>::one(x + single), single);
-    __syncthreads();
+  }
+  __syncthreads();
+  if (parts > 1) cluster_wait();
+  if (warp == LP_WARPS - 1) {
+    const float ps = warp_sum(lane < LP_WARPS ? s_red[1][lane % LP_WARPS] : 0.f), pw = warp_sum(lane < LP_WARPS ? s_red[2][lane % LP_WARPS] : 0.f);
+    if (lane == 0) *in_first(&s_stats[rank], parts) = LpStats{most, ps, pw};
+  }
+  unsigned long long* list = in_first(s_lists[rank], parts);
+  if (n > 0) {
     const int count = s_count;
-    if (tid < n) s_top[tid] = 0;
-    __syncthreads();
     if (count <= LP_CAP) {
       for (int i = tid; i < count; i += LP_THREADS) {
         const unsigned long long k = s_cand[i];
         int better = 0;
+#pragma unroll 4
         for (int j = 0; j < count; ++j) better += s_cand[j] > k;
-        if (better < n) s_top[better] = k;
+        if (better < (n + 3) / 4 * 4) list[better] = k;
       }
+      if (tid >= count && tid < (n + 3) / 4 * 4) list[tid] = 0;  // in fours, as they are compared
     } else {
       // More elements at the bound than there is room for (a row of equal values): the best of all, n times, where each time only
       // the thread that had it looks for its next.
@@ -407,7 +460,11 @@ logprobs_kernel(const LogprobArgs a) {
         if (lane == 0) s_best[warp] = k;
         __syncthreads();
         for (int j = 0; j < LP_WARPS; ++j) k = max(k, s_best[j]);
-        if (tid == 0) s_top[i] = k;
+        if (tid == 0) {
+          list[i] = k;
+          if (i == n - 1)
+            for (int j = n; j % 4; ++j) list[j] = 0;
+        }
         last = k;
         if (extra == k) extra = 0;
         const uint32_t whose = __ballot_sync(0xffffffffu, best == k && k != 0);
@@ -422,84 +479,82 @@ logprobs_kernel(const LogprobArgs a) {
   }
 
   // ---- the parts of the row, joined by the first CTA
-  if (parts > 1) cluster.sync();
-  else __syncthreads();
-  if (rank == 0) {
-    LpStats all = s_stats;
-    if (parts > 1) {
-      for (int r = 1; r < parts; ++r) {
-        const LpStats o = *cluster.map_shared_rank(&s_stats, r);
-        if (o.m > all.m) {
-          const float d = fmaxf(all.m - o.m, LP_FAR), g = all.m > -INFINITY ? lp_ex2(d * LOG2E) : 0.f;
-          const float w1 = all.m > -INFINITY ? g * (all.w + (1.f + all.s) * d) : 0.f;
-          all = LpStats{o.m, o.s + g * (1.f + all.s), o.w + w1};
-        } else if (o.m > -INFINITY) {
-          const float d = fmaxf(o.m - all.m, LP_FAR), g = lp_ex2(d * LOG2E);
-          all.s += g * (1.f + o.s);
-          all.w += g * (o.w + (1.f + o.s) * d);
-        }
-        if (o.s != o.s) all.s = NAN;
-      }
-    }
-    const bool sound = all.m > -INFINITY && all.m < INFINITY && all.s == all.s;
-    const float log_s = sound ? log1pf(all.s) : NAN;
-    if (tid == 0) {
+  if (parts > 1) {
+    cluster_arrive();
+    cluster_wait();
+    if (rank != 0) return;  // nobody reads this CTA's memory
+  } else {
+    __syncthreads();
+  }
+  if (warp == 0) {
+    const bool have = lane < parts;
+    const LpStats o = have ? s_stats[lane % LP_PARTS] : LpStats{-INFINITY, 0.f, 0.f};
+    const float top = warp_max(o.m);
+    const uint32_t these = __ballot_sync(0xffffffffu, have && o.m == top);
+    const float d = fmaxf(o.m - top, LP_FAR), g = o.m > -INFINITY ? lp_ex2(d * LOG2E) : 0.f, full = 1.f + o.s;
+    // a CTA with nothing above -inf still says whether it met a NaN
+    const float s_all = warp_sum(o.m > -INFINITY ? g * (lane == __ffs(these) - 1 ? o.s : full) : o.s == o.s ? 0.f : o.s);
+    const float w_all = warp_sum(o.m > -INFINITY ? g * (o.w + full * d) : 0.f);
+    const bool sound = top > -INFINITY && top < INFINITY && s_all == s_all;
+    const float log_s = sound ? log1pf(s_all) : NAN;
+    if (lane == 0) {
       bool bad_target = false;
       if (a.targets) {
-        const int t = __ldcg(a.targets + row);
-        bad_target = t >= a.vocab;
-        if (a.logprob) a.logprob[row] = t < 0 ? 0.f : bad_target ? NAN : (Logit<T>::one(x + t) - all.m) - log_s;
+        bad_target = target >= a.vocab;
+        a.logprob[row] = target < 0 ? 0.f : bad_target ? NAN : (target_logit - top) - log_s;
       }
-      if (a.entropy) a.entropy[row] = sound ? log_s - all.w / (1.f + all.s) : NAN;
+      if (a.entropy) a.entropy[row] = sound ? log_s - w_all / (1.f + s_all) : NAN;
       if (!sound || bad_target) atomicOr(a.status, (sound ? 0u : A3_DEV_NONFINITE_SCORE) | (bad_target ? A3_DEV_BAD_POSITION : 0u));
-    }
-    if (a.n_top > 0) {
-      const int n = a.n_top;
-      if (parts > 1) {  // the CTAs' lists, ranked by counting
-        const int total = parts * n;
-        for (int i = tid; i < total; i += LP_THREADS) s_cand[i] = cluster.map_shared_rank(s_top, i / n)[i % n];
-        __syncthreads();
-        if (tid < n) s_top[tid] = 0;  // read by this CTA alone
-        __syncthreads();
-        for (int i = tid; i < total; i += LP_THREADS) {
-          const unsigned long long k = s_cand[i];
-          int better = 0;
-          for (int j = 0; j < total; ++j) better += s_cand[j] > k;
-          if (k != 0 && better < n) s_top[better] = k;
-        }
-        __syncthreads();
-      }
-      if (warp == 0) {
-        // fewer elements above -inf than asked for: the lowest ids of those at -inf, then of NaNs
-        int have = __popc(__ballot_sync(0xffffffffu, lane < n && s_top[lane < n ? lane : 0] != 0));
-        for (int pass = 0; pass < 2 && have < n; ++pass) {
-          for (int i0 = 0; i0 < a.vocab && have < n; i0 += 32) {
-            const int i = i0 + lane;
-            const uint32_t o = i < a.vocab ? ordered(Logit<T>::one(x + i)) : 0xffffffffu;
-            const uint32_t these = __ballot_sync(0xffffffffu, o == (pass == 0 ? LP_NONE : 0u));
-            const int at = have + __popc(these & ((1u << lane) - 1));
-            if ((these >> lane & 1) && at < n) s_top[at] = lp_key(o, i);
-            have = min(n, have + __popc(these));
-            __syncwarp();
-          }
-        }
-        __syncwarp();
-        if (lane < n) {
-          const unsigned long long k = s_top[lane];
-          a.top_ids[(long long)row * n + lane] = key_id(k);
-          a.top_logprobs[(long long)row * n + lane] = sound ? (unordered((uint32_t)(k >> 32)) - all.m) - log_s : NAN;
-        }
-      }
+      s_red[0][0] = top;
+      s_red[1][0] = log_s;
     }
   }
-  if (parts > 1) cluster.sync();  // nobody leaves while its shared memory is read
+  if (n == 0) return;
+  if (tid < n) s_top[tid] = parts == 1 ? s_lists[0][tid] : 0;
+  __syncthreads();
+  const float top = s_red[0][0], log_s = s_red[1][0];  // log_s: NaN where there is no distribution
+  if (parts > 1) {  // an element's place is how many are better: all of them compared, which needs no branch
+    for (int i = tid; i < parts * n; i += LP_THREADS) {
+      const unsigned long long k = s_lists[i / n][i % n];
+      int better = k == 0 ? n : 0;
+#pragma unroll 1
+      for (int l = 0; l < parts; ++l)
+#pragma unroll 1
+        for (int j = 0; j < n; j += 4)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) better += s_lists[l][j + e] > k;
+      if (better < n) s_top[better] = k;
+    }
+    __syncthreads();
+  }
+  if (warp == 0) {
+    // fewer elements above -inf than asked for: the lowest ids of those at -inf, then of NaNs
+    int have = __popc(__ballot_sync(0xffffffffu, lane < n && s_top[lane] != 0));
+    for (int pass = 0; pass < 2 && have < n; ++pass) {
+      for (int i0 = 0; i0 < a.vocab && have < n; i0 += 32) {
+        const int i = i0 + lane;
+        const uint32_t o = i < a.vocab ? ordered(Logit<T>::one(x + i)) : 0xffffffffu;
+        const uint32_t these = __ballot_sync(0xffffffffu, o == (pass == 0 ? LP_NONE : 0u));
+        const int at = have + __popc(these & ((1u << lane) - 1));
+        if ((these >> lane & 1) && at < n) s_top[at] = lp_key(o, i);
+        have = min(n, have + __popc(these));
+        __syncwarp();
+      }
+    }
+    __syncwarp();
+    if (lane < n) {
+      const unsigned long long k = s_top[lane];
+      a.top_ids[(long long)row * n + lane] = key_id(k);
+      a.top_logprobs[(long long)row * n + lane] = log_s == log_s ? (unordered((uint32_t)(k >> 32)) - top) - log_s : NAN;
+    }
+  }
 }
 
 template <typename T>
 static int logprobs_launch(const a3_handle* h, const LogprobArgs& a, cudaStream_t st) {
-  // CTAs per row: as many as the device holds, and no fewer than 2 048 elements for each
+  // CTAs per row: two for each SM (more of them cost more at their ends than they save: 65 rows of 152 064 in bf16, 4 CTAs 14.2 us, 8 17.2), and no fewer than 2 048 elements for each
   int parts = 1;
-  while (parts < 8 && (long long)a.M * parts * 2 <= LP_MIN * h->sm_count && a.vocab / (2 * parts) >= 2048) parts *= 2;
+  while (parts < LP_PARTS && (long long)a.M * parts * 2 <= 2 * h->sm_count && a.vocab / (2 * parts) >= 2048) parts *= 2;
   if ((long long)a.M * parts > 0x7fffffffll) return A3_EINVAL;
   static SmemAttrOnce once;
   A3_TRY(smem_attr_once(once, h->device, logprobs_kernel<T>, LP_RING));
