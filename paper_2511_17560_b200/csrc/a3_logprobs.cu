@@ -74,6 +74,7 @@ template <>
 struct Logit<float> {
   static constexpr int VE = 4;
   static constexpr float LOWEST = -3.40282347e38f;
+  static constexpr uint32_t NONE = 0xff800000u;
   __device__ static uint4 max_of(uint4 a, uint4 b) { return make_uint4(two(a.x, b.x), two(a.y, b.y), two(a.z, b.z), two(a.w, b.w)); }
   __device__ static uint32_t two(uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }
   __device__ static float largest(uint4 v) { return __uint_as_float(two(two(v.x, v.y), two(v.z, v.w))); }
@@ -90,6 +91,7 @@ template <>
 struct Logit<bf16> {
   static constexpr int VE = 8;
   static constexpr float LOWEST = -3.38953139e38f;
+  static constexpr uint32_t NONE = 0xff80ff80u;  // a word of -inf
   __device__ static uint4 max_of(uint4 a, uint4 b) { return make_uint4(two(a.x, b.x), two(a.y, b.y), two(a.z, b.z), two(a.w, b.w)); }
   __device__ static uint32_t two(uint32_t a, uint32_t b) {
     uint32_t y;
@@ -112,6 +114,7 @@ template <>
 struct Logit<__half> {
   static constexpr int VE = 8;
   static constexpr float LOWEST = -65504.f;
+  static constexpr uint32_t NONE = 0xfc00fc00u;
   __device__ static uint4 max_of(uint4 a, uint4 b) { return make_uint4(two(a.x, b.x), two(a.y, b.y), two(a.z, b.z), two(a.w, b.w)); }
   __device__ static uint32_t two(uint32_t a, uint32_t b) {
     uint32_t y;
@@ -257,32 +260,34 @@ logprobs_kernel(const LogprobArgs a) {
         if (f[i] != f[i]) s = NAN;
     }
   };
-  // Vectors at hand at once: one look at whether the maximum rises.  With a maximum in the ordinary range -inf may stand as the type's
-  // lowest number: its exponential is 0 and the product of the two is.
-  auto take = [&](const uint4* at, int n) {  // at, at + LP_THREADS, ...: n of them
+  // LP_U vectors at once (at, at + LP_THREADS, ...; from the n-th on -inf): one look at whether the maximum rises.  With a maximum in the
+  // ordinary range -inf may stand as the type's lowest number: its exponential is 0 and the product of the two is.
+  auto take = [&](const uint4* at, int n) {
     uint4 raw[LP_U];
 #pragma unroll
-    for (int u = 0; u < LP_U; ++u) raw[u] = at[u * LP_THREADS];  // behind the n-th: not used
+    for (int u = 0; u < LP_U; ++u) raw[u] = at[u * LP_THREADS];
+    if (n < LP_U) {
+#pragma unroll
+      for (int u = 0; u < LP_U; ++u)
+        if (u >= n) raw[u] = make_uint4(Logit<T>::NONE, Logit<T>::NONE, Logit<T>::NONE, Logit<T>::NONE);
+    }
     uint4 top = raw[0];
 #pragma unroll
-    for (int u = 1; u < LP_U; ++u)
-      if (u < n) top = Logit<T>::max_of(top, raw[u]);
+    for (int u = 1; u < LP_U; ++u) top = Logit<T>::max_of(top, raw[u]);
     raise(Logit<T>::largest(top));
     if (m > Logit<T>::LOWEST && m < 1e30f) {
       const f32x2 ref = pack_f2(-m, -m), log2e = pack_f2(LOG2E, LOG2E);
 #pragma unroll
       for (int u = 0; u < LP_U; ++u) {
-        if (u < n) {
-          f32x2 p[VE / 2];
-          Logit<T>::pairs(raw[u], p);
+        f32x2 p[VE / 2];
+        Logit<T>::pairs(raw[u], p);
 #pragma unroll
-          for (int i = 0; i < VE / 2; ++i) {
-            const f32x2 d = add_f2(p[i], ref);
-            const float2 t = unpack_f2(mul_f2(d, log2e));
-            const f32x2 e = pack_f2(lp_ex2(t.x), lp_ex2(t.y));
-            s2 = add_f2(s2, e);
-            w2 = fma_f2(e, d, w2);
-          }
+        for (int i = 0; i < VE / 2; ++i) {
+          const f32x2 d = add_f2(p[i], ref);
+          const float2 t = unpack_f2(mul_f2(d, log2e));
+          const f32x2 e = pack_f2(lp_ex2(t.x), lp_ex2(t.y));
+          s2 = add_f2(s2, e);
+          w2 = fma_f2(e, d, w2);
         }
       }
     } else {
@@ -297,22 +302,32 @@ logprobs_kernel(const LogprobArgs a) {
   {
     // Each thread's vectors come through a ring of its own in shared memory, LP_STAGES - 1 batches under way while one is computed: what the
     // registers of all threads hold is too little to cover the way from HBM.
-    const uint32_t mine_u = smem_u32(ring + tid);
     constexpr int BATCH = LP_THREADS * LP_U;
-    auto fetch = [&](int b) {
-      const int v = v0 + tid + b * BATCH;
+    const uint32_t ring_u = smem_u32(ring + tid);
+    const uint4* from = xv + v0 + tid;
+    int to_fetch = v1 - v0, left = v1 - v0;  // vectors of the CTA
+    uint32_t put = 0, get = 0;               // batches of the ring, in bytes
+    auto turn = [](uint32_t& at) { at = at == (LP_STAGES - 1) * BATCH * 16 ? 0 : at + BATCH * 16; };
+    auto fetch = [&] {
+      if (to_fetch >= BATCH) {
 #pragma unroll
-      for (int u = 0; u < LP_U; ++u)
-        if (v + u * LP_THREADS < v1) cp_async16(mine_u + (b % LP_STAGES * BATCH + u * LP_THREADS) * 16, xv + v + u * LP_THREADS, true);
+        for (int u = 0; u < LP_U; ++u) cp_async16(ring_u + put + u * LP_THREADS * 16, from + u * LP_THREADS, true);
+      } else {
+#pragma unroll
+        for (int u = 0; u < LP_U; ++u)
+          if (tid + u * LP_THREADS < to_fetch) cp_async16(ring_u + put + u * LP_THREADS * 16, from + u * LP_THREADS, true);
+      }
       cp_async_commit();
+      from += BATCH, to_fetch -= BATCH;
+      turn(put);
     };
 #pragma unroll 1
-    for (int b = 0; b < LP_STAGES - 1; ++b) fetch(b);
-    int b = 0;
-    for (int v = v0 + tid; v < v1; v += BATCH, ++b) {
-      fetch(b + LP_STAGES - 1);
+    for (int b = 0; b < LP_STAGES - 1; ++b) fetch();
+    for (; left > 0; left -= BATCH) {
+      fetch();
       cp_async_wait<LP_STAGES - 1>();
-      take(ring + tid + b % LP_STAGES * BATCH, min(LP_U, (v1 - v + LP_THREADS - 1) / LP_THREADS));
+      take(reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(ring + tid) + get), left >= BATCH ? LP_U : (left - tid + LP_THREADS - 1) / LP_THREADS);
+      turn(get);
     }
   }
   {
