@@ -214,7 +214,6 @@ logprobs_kernel(const LogprobArgs a) {
   const int parts = (int)cluster_size(), rank = (int)cluster_rank();
   if (parts > 1) cluster_arrive();  // waited for before the first access to another CTA's memory: it has to be there
   pdl_wait();
-  pdl_launch_dependents();
   const int row = blockIdx.x / parts, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const T* x = reinterpret_cast<const T*>(a.logits) + row * a.row_stride;
   // 16-byte vectors from the first boundary on, the few elements before and behind them one by one
@@ -336,6 +335,7 @@ logprobs_kernel(const LogprobArgs a) {
     w += ww.x + ww.y;
     s2 = w2 = 0;
   }
+  pdl_launch_dependents();
   const uint32_t mine = ordered(m);  // of the vectors alone; LP_NONE: nothing above -inf
   if (single >= 0) {
     const float f = Logit<T>::one(x + single);
@@ -573,7 +573,24 @@ static int logprobs_launch(const a3_handle* h, const LogprobArgs& a, cudaStream_
   if ((long long)a.M * parts > 0x7fffffffll) return A3_EINVAL;
   static SmemAttrOnce once;
   A3_TRY(smem_attr_once(once, h->device, logprobs_kernel<T>, LP_RING));
-  A3_CUDA(launch_pdl_cluster(parts, logprobs_kernel<T>, dim3((unsigned)(a.M * parts)), dim3(LP_THREADS), LP_RING, st, a));
+  const dim3 grid((unsigned)(a.M * parts));
+  if (parts == 1) {
+    A3_CUDA(launch_pdl(logprobs_kernel<T>, grid, dim3(LP_THREADS), LP_RING, st, a));
+    return launched();
+  }
+  // Clusters wait for the launch before them: started beside it they took 19.4 us for 65 rows of 152 064 where they take 16.5 so, and 14.5 alone.
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(LP_THREADS);
+  cfg.dynamicSmemBytes = LP_RING;
+  cfg.stream = st;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = (unsigned)parts;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  A3_CUDA(cudaLaunchKernelEx(&cfg, logprobs_kernel<T>, a));
   return launched();
 }
 
