@@ -388,41 +388,68 @@ typedef struct {
  * [heads][D] without gaps.  row_seq[r] < 0 marks padding: nothing of such a row is written.  A row whose sequence, slot, page or
  * |pos| is out of range (n_seqs, max_pages, n_pages, max_positions) is left out as a whole and A3_DEV_BAD_POSITION is set.  Rows of
  * one call must go to different slots.  One launch. */
-int a3_paged_append(const a3_handle* h, const a3_paged_cache* cache, const int32_t* page_table, int n_seqs, int max_pages,
-                    const int32_t* row_seq, const int32_t* row_slot, const int32_t* row_pos, int rotate, const void* q_rows,
-                    size_t q_stride, const void* k_rows, size_t k_stride, const void* v_rows, size_t v_stride, int M, void* q_out,
-                    size_t q_out_stride, a3_stream stream);
+typedef struct {
+  const int32_t* page_table;  /* dev [n_seqs][max_pages] */
+  const int32_t* row_seq;     /* dev [M] */
+  const int32_t* row_slot;    /* dev [M] */
+  const int32_t* row_pos;     /* dev [M] or NULL */
+  const void* q_rows;         /* dev, 16-byte aligned, as all rows here, or NULL */
+  const void* k_rows;
+  const void* v_rows;
+  void* q_out;
+  uint64_t q_stride, k_stride, v_stride, q_out_stride; /* elements */
+  int32_t n_seqs, max_pages, M, rotate;
+} a3_paged_rows;
+int a3_paged_append(const a3_handle* h, const a3_paged_cache* cache, const a3_paged_rows* rows, a3_stream stream);
 
 /* Attention of one new token per sequence over its pages:
  *   out[s][h] = sum over t < cache_len[s] of Softmax_t(scale * q[s][h] . k[s][t][h/G]) v[s][t][h/G],  G = Hq/Hkv
- * q_rows: dev [n_seqs][Hq][D] bf16, rotated, q_stride elements (a multiple of 8) between sequences; cache_len: dev [n_seqs], the new
- * token's own slot included; out: dev [n_seqs][Hq][D] bf16; lse_out: dev [n_seqs][Hq] fp32 natural-log row log-sum-exps of the scaled
- * logits, or NULL.  A sequence of length 0 (padding of a batch of fixed size) gives zeros and -inf.  A length below 0 or above
- * max_pages*page_size counts as 0, keys and values of a page outside [0, n_pages) count as zeros, and both set A3_DEV_BAD_POSITION.
- * A3_ETOOLARGE: max_pages*page_size above 2^31 - 2^16, or n_seqs times that above 2^34.  Lengths are read on the device only, so a captured call follows them.  The result is deterministic.
- * ws: dev, 256-byte aligned, a3_paged_attention_workspace_bytes(h) bytes, borrowed until the call's kernels have ended; needs
- * no clearing.  Two launches, no allocation, no synchronisation. */
+ * with q_rows rotated and the new token's own slot counted in cache_len.  A sequence of length 0 (padding of a batch of fixed size)
+ * gives zeros and -inf.  A length below 0 or above max_pages*page_size counts as 0, keys and values of a page outside [0, n_pages) count
+ * as zeros, and both set A3_DEV_BAD_POSITION.  A3_ETOOLARGE: max_pages*page_size above 2^31 - 2^16, or n_seqs times that above
+ * 2^34.  Lengths are read on the device only, so a captured call follows them.  The result is deterministic.
+ * The workspace is borrowed until the call's kernels have ended and needs no clearing.  At most two launches, no allocation, no
+ * synchronisation. */
+typedef struct {
+  const int32_t* page_table; /* dev [n_seqs][max_pages] */
+  const int32_t* cache_len;  /* dev [n_seqs] */
+  const void* q_rows;        /* dev [n_seqs][Hq][D] bf16, 16-byte aligned */
+  void* out;                 /* dev [n_seqs][Hq][D] bf16, 16-byte aligned */
+  float* lse_out;            /* dev [n_seqs][Hq] natural-log row log-sum-exps of the scaled logits, or NULL */
+  void* ws;                  /* dev, 256-byte aligned, a3_paged_attention_workspace_bytes(h) bytes */
+  uint64_t ws_bytes;
+  uint64_t q_stride;         /* elements between sequences, a multiple of 8 */
+  int32_t n_seqs, max_pages;
+  float scale;
+  int32_t reserved;
+} a3_paged_queries;
 size_t a3_paged_attention_workspace_bytes(const a3_handle* h);
-int a3_paged_attention(const a3_handle* h, const a3_paged_cache* cache, const int32_t* page_table, int n_seqs, int max_pages,
-                       const int32_t* cache_len, const void* q_rows, size_t q_stride, float scale, void* out, float* lse_out, void* ws,
-                       size_t ws_bytes, a3_stream stream);
+int a3_paged_attention(const a3_handle* h, const a3_paged_cache* cache, const a3_paged_queries* queries, a3_stream stream);
 
 /* Log probabilities of given tokens, entropies and the best alternatives, from rows of logits (a3_first_token's, or a projection of
  * many rows): with lse = log sum_i exp(x_i),
  *   logprob_out[m] = x[targets[m]] - lse,   entropy_out[m] = -sum_i p_i log p_i (natural logarithm; p_i = 0 adds nothing),
  *   top_ids_out[m][j], top_logprobs_out[m][j]: the n_top largest in descending order, ties to the lower id.
- * logits: dev [M][vocab] of `type`, row_stride elements between rows, no alignment beyond the element's.  targets: dev [M]
- * int32 or NULL (then no logprob_out); a negative target (padding) gives 0, one beyond the vocabulary NaN and
- * A3_DEV_BAD_POSITION.  -inf logits (tokens ruled out) are ordinary values.  A row with a NaN or +inf, or with nothing but -inf, has no
- * distribution: its log probabilities and entropy are NaN and A3_DEV_NONFINITE_SCORE is set; NaNs come last among the alternatives.
- * logprob_out and entropy_out: dev [M] fp32 or NULL; top_*_out: dev [M][n_top], NULL iff n_top = 0; n_top <= A3_LOGPROBS_MAX_TOP and
- * n_top <= vocab.  One launch, no workspace. */
+ * A negative target (padding) gives 0, one beyond the vocabulary NaN and A3_DEV_BAD_POSITION.  -inf logits (tokens ruled out) are
+ * ordinary values.  A row with a NaN or +inf, or with nothing but -inf, has no distribution: its log probabilities and entropy are NaN and
+ * A3_DEV_NONFINITE_SCORE is set; NaNs come last among the alternatives.  n_top <= A3_LOGPROBS_MAX_TOP and n_top <= vocab.
+ * One launch, no workspace. */
 #define A3_LOGPROBS_MAX_TOP 32
 #define A3_LOGITS_FP32 0
 #define A3_LOGITS_BF16 1
 #define A3_LOGITS_FP16 2
-int a3_token_logprobs(const a3_handle* h, const void* logits, int type, size_t row_stride, int M, int vocab, const int32_t* targets,
-                      int n_top, float* logprob_out, float* entropy_out, int32_t* top_ids_out, float* top_logprobs_out, a3_stream stream);
+typedef struct {
+  const void* logits;       /* dev [M][vocab] of `type`, aligned as its elements are */
+  const int32_t* targets;   /* dev [M], or NULL together with logprob_out */
+  float* logprob_out;       /* dev [M] */
+  float* entropy_out;       /* dev [M] or NULL */
+  int32_t* top_ids_out;     /* dev [M][n_top], NULL iff n_top = 0 */
+  float* top_logprobs_out;  /* likewise */
+  uint64_t row_stride;      /* elements */
+  int32_t type;             /* A3_LOGITS_* */
+  int32_t M, vocab, n_top;
+} a3_logit_rows;
+int a3_token_logprobs(const a3_handle* h, const a3_logit_rows* rows, a3_stream stream);
 
 /* Waits for `stream`, reads and clears the device status word (A3_DEV_* bits). */
 int a3_device_status(const a3_handle* h, uint32_t* bits_out, a3_stream stream);

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Dict, List, Optional, Sequence
 
 import numpy as np
@@ -129,11 +130,11 @@ def _load():
     lib.a3_first_token_workspace_bytes.argtypes = [vp]
     lib.a3_first_token_workspace_bytes.restype = sz
     lib.a3_first_token.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, sz, vp]
-    lib.a3_paged_append.argtypes = [vp, C.POINTER(PagedCacheDesc), vp, i32, i32, vp, vp, vp, i32, vp, sz, vp, sz, vp, sz, i32, vp, sz, vp]
+    lib.a3_paged_append.argtypes = [vp, vp, C.c_char_p, vp]
     lib.a3_paged_attention_workspace_bytes.argtypes = [vp]
     lib.a3_paged_attention_workspace_bytes.restype = sz
-    lib.a3_paged_attention.argtypes = [vp, C.POINTER(PagedCacheDesc), vp, i32, i32, vp, vp, sz, C.c_float, vp, vp, vp, sz, vp]
-    lib.a3_token_logprobs.argtypes = [vp, vp, i32, sz, i32, i32, vp, i32, vp, vp, vp, vp, vp]
+    lib.a3_paged_attention.argtypes = [vp, vp, C.c_char_p, vp]
+    lib.a3_token_logprobs.argtypes = [vp, C.c_char_p, vp]
     lib.a3_fuse_request.argtypes = [vp, C.POINTER(Request), vp, sz, vp]
     lib.a3_fuse_batch.argtypes = [vp, C.POINTER(Request), i32, vp, sz, vp]
     lib.a3_fuse_request_host.argtypes = [vp, C.POINTER(Request), C.POINTER(HostIO), vp, sz, vp, sz, vp]
@@ -284,9 +285,14 @@ class PagedCache:
         stride = k_pages.stride(0) if n > 1 else size * heads * d
         self.desc = PagedCacheDesc(k_pages.data_ptr(), v_pages.data_ptr(), stride * k_pages.element_size(), n, size, 1 if packed else 0, 0,
                                    _ptr(k_scale), _ptr(v_scale))
-        self._ref = C.byref(self.desc)
+        self._ref = C.addressof(self.desc)
 
 
+# a3_paged_rows, a3_paged_queries and a3_logit_rows as one call's bytes: these calls are short on the device, and packing the
+# fields at once takes half the time of a ctypes argument each
+PAGED_ROWS = struct.Struct("@8P4Q4i")
+PAGED_QUERIES = struct.Struct("@6P2Q2ifi")
+LOGIT_ROWS = struct.Struct("@6PQ4i")
 _LOGIT_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
@@ -443,103 +449,105 @@ class A3:
                                       _ptr(ws), ws.numel(), _stream()), "a3_first_token")
         return logits, token
 
-    # ---- decoding on paged caches (these calls are short on the device: each check is made once, and no text is built before it is needed)
-    def _ints(self, where, t, shape):
-        """Address of an int32 tensor of this shape on the engine's device."""
-        if t.dtype is not torch.int32 or t.shape != shape or t.device != self.device or not t.is_contiguous():
-            raise A3Error(-1, where + ": int32 indices on the engine's device")
-        return t.data_ptr()
-
-    def _rows(self, where, t, shape):
-        """Address of bf16 rows of this shape [n][heads][D], whose heads lie next to each other, and the elements between them."""
-        if t.dtype is not torch.bfloat16 or t.shape != shape or t.device != self.device:
-            raise A3Error(-1, where + ": bf16 rows on the engine's device")
-        n, heads, d = shape
-        row, head, one = t.stride()
-        if n > 0 and (one != 1 or (head != d and heads > 1)):
-            raise A3Error(-1, where + ": the heads of a row lie next to each other")
-        return t.data_ptr(), row if n > 1 else heads * d
-
-    def _paged(self, where, cache, page_table):
-        m = self.shape
-        if cache.n_kv_heads != m.n_kv_heads or cache.head_dim != m.head_dim or cache.device != self.device or page_table.dim() != 2:
-            raise A3Error(-1, where + ": cache of another model or device, or no page table")
-        return page_table.shape
-
+    # ---- decoding on paged caches (these calls are short on the device: one condition for all that must hold, and no text before it fails)
     def paged_append(self, cache: PagedCache, page_table, row_seq, row_slot, k_rows, v_rows, q_rows=None, row_pos=None, rotate=True, q_out=None):
         """a3_paged_append; page_table [n_seqs][max_pages], rows [M][heads][D] (columns of a wider buffer will do); returns q_out or None."""
-        where, m = "a3_paged_append", self.shape
-        table_shape = n_seqs, max_pages = self._paged(where, cache, page_table)
-        rows = row_seq.shape
-        if len(rows) != 1:
-            raise A3Error(-1, where + ": row_seq")
-        M, D = rows[0], m.head_dim
+        m, dev, i32, bf16 = self.shape, self.device, torch.int32, torch.bfloat16
+        rows, D = row_seq.shape, m.head_dim
+        if not (len(rows) == 1 and page_table.dim() == 2 and cache.n_kv_heads == m.n_kv_heads and cache.head_dim == D and cache.device == dev
+                and row_slot.shape == rows and page_table.dtype is row_seq.dtype is row_slot.dtype is i32
+                and page_table.device == dev and row_seq.device == dev and row_slot.device == dev
+                and page_table.is_contiguous() and row_seq.is_contiguous() and row_slot.is_contiguous()):
+            raise A3Error(-1, "a3_paged_append: cache of this model, and contiguous int32 page table and rows, on the engine's device")
+        if row_pos is not None and not (row_pos.shape == rows and row_pos.dtype is i32 and row_pos.device == dev and row_pos.is_contiguous()):
+            raise A3Error(-1, "a3_paged_append: row_pos")
+        M, = rows
         kv_shape = (M, m.n_kv_heads, D)
-        k, ks = self._rows(where, k_rows, kv_shape)
-        v, vs = self._rows(where, v_rows, kv_shape)
-        q = out = None
-        qs = os = 0
+        kr, kh, ke = k_rows.stride()
+        vr, vh, ve = v_rows.stride()
+        if not (k_rows.shape == kv_shape and v_rows.shape == kv_shape and k_rows.dtype is v_rows.dtype is bf16 and k_rows.device == dev
+                and v_rows.device == dev and (M == 0 or (ke == ve == 1 and (kh == vh == D or m.n_kv_heads == 1)))):
+            raise A3Error(-1, "a3_paged_append: k_rows, v_rows: bf16 [M][Hkv][D] on the engine's device, the heads of a row next to each other")
+        q = out = qr = outr = 0
         if q_rows is not None:
             q_shape = (M, m.n_q_heads, D)
-            q, qs = self._rows(where, q_rows, q_shape)
             if q_out is None:
                 q_out = q_rows.new_empty(q_shape)
-            out, os = self._rows(where, q_out, q_shape)
+            qr, qh, qe = q_rows.stride()
+            outr, oh, oe = q_out.stride()
+            if not (q_rows.shape == q_shape and q_out.shape == q_shape and q_rows.dtype is q_out.dtype is bf16 and q_rows.device == dev
+                    and q_out.device == dev and (M == 0 or (qe == oe == 1 and (qh == oh == D or m.n_q_heads == 1)))):
+                raise A3Error(-1, "a3_paged_append: q_rows, q_out: bf16 [M][Hq][D] on the engine's device, the heads of a row next to each other")
+            q, out = q_rows.data_ptr(), q_out.data_ptr()
         elif q_out is not None:
-            raise A3Error(-1, where + ": q_out without q_rows")
-        status = _load().a3_paged_append(self._h, cache._ref, self._ints(where, page_table, table_shape), n_seqs, max_pages, self._ints(where, row_seq, rows),
-                                         self._ints(where, row_slot, rows), None if row_pos is None else self._ints(where, row_pos, rows),
-                                         1 if rotate else 0, q, qs, k, ks, v, vs, M, out, os, _stream())
+            raise A3Error(-1, "a3_paged_append: q_out without q_rows")
+        if M == 1:  # one row has no distance to the next
+            kr = vr = m.n_kv_heads * D
+            qr = outr = m.n_q_heads * D
+        status = _load().a3_paged_append(self._h, cache._ref, PAGED_ROWS.pack(
+            page_table.data_ptr(), row_seq.data_ptr(), row_slot.data_ptr(), 0 if row_pos is None else row_pos.data_ptr(), q, k_rows.data_ptr(),
+            v_rows.data_ptr(), out, qr, kr, vr, outr, *page_table.shape, M, 1 if rotate else 0), _stream())
         if status != A3_OK:
-            raise A3Error(status, where)
+            raise A3Error(status, "a3_paged_append")
         return q_out
 
     def paged_attention(self, cache: PagedCache, page_table, cache_len, q_rows, scale=None, out=None, want_lse=False):
         """a3_paged_attention; returns (out [n_seqs][Hq][D], lse [n_seqs][Hq] or None).  The workspace is allocated by torch for
         this call alone, so that calls on several streams, or captured into several graphs, share none."""
-        where, m, lib = "a3_paged_attention", self.shape, _load()
-        table_shape = n, max_pages = self._paged(where, cache, page_table)
-        heads = m.n_q_heads
-        shape = (n, heads, m.head_dim)
-        q, qs = self._rows(where, q_rows, shape)
+        m, dev, lib = self.shape, self.device, _load()
+        Hq, D = m.n_q_heads, m.head_dim
+        if not (page_table.dim() == 2 and cache_len.dim() == 1 and cache.n_kv_heads == m.n_kv_heads and cache.head_dim == D and cache.device == dev
+                and page_table.dtype is cache_len.dtype is torch.int32 and page_table.device == dev and cache_len.device == dev
+                and page_table.is_contiguous() and cache_len.is_contiguous()):
+            raise A3Error(-1, "a3_paged_attention: cache of this model, and contiguous int32 page table and lengths, on the engine's device")
+        n, max_pages = page_table.shape
+        shape = (n, Hq, D)
+        qr, qh, qe = q_rows.stride()
+        if not (cache_len.shape[0] == n and q_rows.shape == shape and q_rows.dtype is torch.bfloat16 and q_rows.device == dev
+                and (n == 0 or (qe == 1 and (qh == D or Hq == 1)))):
+            raise A3Error(-1, "a3_paged_attention: q_rows: bf16 [n_seqs][Hq][D] on the engine's device, the heads of a row next to each other")
         if out is None:
             out = torch.empty_like(q_rows, memory_format=torch.contiguous_format)
-        elif out.dtype is not torch.bfloat16 or out.shape != shape or not out.is_contiguous() or out.device != self.device:
-            raise A3Error(-1, where + ": out")
-        lse = q_rows.new_empty((n, heads), dtype=torch.float32) if want_lse else None
+        elif not (out.dtype is torch.bfloat16 and out.shape == shape and out.is_contiguous() and out.device == dev):
+            raise A3Error(-1, "a3_paged_attention: out")
+        lse = q_rows.new_empty((n, Hq), dtype=torch.float32) if want_lse else None
         nbytes = lib.a3_paged_attention_workspace_bytes(self._h)
         ws = q_rows.new_empty(nbytes, dtype=torch.uint8)
-        status = lib.a3_paged_attention(self._h, cache._ref, self._ints(where, page_table, table_shape), n, max_pages, self._ints(where, cache_len, (n,)), q, qs,
-                                        m.head_dim ** -0.5 if scale is None else scale, out.data_ptr(), None if lse is None else lse.data_ptr(),
-                                        ws.data_ptr(), nbytes, _stream())
+        status = lib.a3_paged_attention(self._h, cache._ref, PAGED_QUERIES.pack(
+            page_table.data_ptr(), cache_len.data_ptr(), q_rows.data_ptr(), out.data_ptr(), 0 if lse is None else lse.data_ptr(), ws.data_ptr(), nbytes,
+            qr if n > 1 else Hq * D, n, max_pages, D ** -0.5 if scale is None else scale, 0), _stream())
         if status != A3_OK:
-            raise A3Error(status, where)
+            raise A3Error(status, "a3_paged_attention")
         return out, lse
 
     def token_logprobs(self, logits, targets=None, n_top=0):
         """a3_token_logprobs on logits [M][vocab] (fp32, bf16 or fp16; rows may be apart); returns (logprob [M] or None without targets,
         entropy [M], top_ids [M][n_top] and top_logprobs [M][n_top], or None)."""
-        where = "a3_token_logprobs"
         kind = _LOGIT_TYPES.get(logits.dtype)
         if kind is None or logits.dim() != 2 or logits.device != self.device:
-            raise A3Error(-1, where + ": logits")
+            raise A3Error(-1, "a3_token_logprobs: logits [M][vocab] on the engine's device")
         M, vocab = logits.shape
         row, one = logits.stride()
         if vocab == 0 or (one != 1 and vocab > 1):
-            raise A3Error(-1, where + ": logits of a row lie next to each other")
-        logprob = ids = lps = t = None
+            raise A3Error(-1, "a3_token_logprobs: logits of a row lie next to each other")
+        logprob = ids = lps = None
+        given = logprob_at = ids_at = lps_at = 0
         if targets is not None:
-            t = self._ints(where, targets, (M,))
+            if not (targets.shape == (M,) and targets.dtype is torch.int32 and targets.device == self.device and targets.is_contiguous()):
+                raise A3Error(-1, "a3_token_logprobs: targets: contiguous int32 [M] on the engine's device")
             logprob = logits.new_empty(M, dtype=torch.float32)
-        entropy = torch.empty_like(logprob) if t else logits.new_empty(M, dtype=torch.float32)
+            entropy = torch.empty_like(logprob)
+            given, logprob_at = targets.data_ptr(), logprob.data_ptr()
+        else:
+            entropy = logits.new_empty(M, dtype=torch.float32)
         if n_top > 0:
             lps = logits.new_empty((M, n_top), dtype=torch.float32)
             ids = torch.empty_like(lps, dtype=torch.int32)
-        status = _load().a3_token_logprobs(self._h, logits.data_ptr(), kind, row if M > 1 else vocab, M, vocab, t, n_top,
-                                           None if logprob is None else logprob.data_ptr(), entropy.data_ptr(),
-                                           None if ids is None else ids.data_ptr(), None if lps is None else lps.data_ptr(), _stream())
+            ids_at, lps_at = ids.data_ptr(), lps.data_ptr()
+        status = _load().a3_token_logprobs(self._h, LOGIT_ROWS.pack(logits.data_ptr(), given, logprob_at, entropy.data_ptr(), ids_at, lps_at,
+                                                                    row if M > 1 else vocab, kind, M, vocab, n_top), _stream())
         if status != A3_OK:
-            raise A3Error(status, where)
+            raise A3Error(status, "a3_token_logprobs")
         return logprob, entropy, ids, lps
 
     def make_request(self, chunks, n_chunks, max_chunk_len, n_ctx, n_question, x0, k_fused, v_fused, ratio=0.15,

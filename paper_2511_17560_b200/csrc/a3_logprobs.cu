@@ -598,20 +598,20 @@ static int logprobs_launch(const a3_handle* h, const LogprobArgs& a, cudaStream_
 
 using namespace a3;
 
-extern "C" int a3_token_logprobs(const a3_handle* h, const void* logits, int type, size_t row_stride, int M, int vocab,
-                                 const int32_t* targets, int n_top, float* logprob_out, float* entropy_out, int32_t* top_ids_out,
-                                 float* top_logprobs_out, a3_stream stream) {
-  if (!h || M < 0 || vocab <= 0 || n_top < 0 || n_top > vocab) return A3_EINVAL;
-  if (n_top > A3_LOGPROBS_MAX_TOP || type < A3_LOGITS_FP32 || type > A3_LOGITS_FP16) return A3_EUNSUPPORTED;
+extern "C" int a3_token_logprobs(const a3_handle* h, const a3_logit_rows* rows, a3_stream stream) {
+  if (!h || !rows) return A3_EINVAL;
+  const a3_logit_rows& p = *rows;
+  if (p.M < 0 || p.vocab <= 0 || p.n_top < 0 || p.n_top > p.vocab) return A3_EINVAL;
+  if (p.n_top > A3_LOGPROBS_MAX_TOP || p.type < A3_LOGITS_FP32 || p.type > A3_LOGITS_FP16) return A3_EUNSUPPORTED;
   int device = -1;
   if (cudaGetDevice(&device) != cudaSuccess || device != h->device) return A3_EINVAL;
-  if (M == 0) return A3_OK;
-  if (!targets != !logprob_out || !top_ids_out != (n_top == 0) || !top_logprobs_out != (n_top == 0)) return A3_EINVAL;
-  if (!logits || (uintptr_t)logits % (type == A3_LOGITS_FP32 ? 4 : 2)) return A3_EINVAL;
-  if ((M > 1 && row_stride < (size_t)vocab) || row_stride > (size_t)1 << 40) return A3_EINVAL;
-  const LogprobArgs a{logits, (long long)row_stride, M, vocab, targets, n_top, logprob_out, entropy_out, top_ids_out, top_logprobs_out, h->dev_status};
+  if (p.M == 0) return A3_OK;
+  if (!p.targets != !p.logprob_out || !p.top_ids_out != (p.n_top == 0) || !p.top_logprobs_out != (p.n_top == 0)) return A3_EINVAL;
+  if (!p.logits || (uintptr_t)p.logits % (p.type == A3_LOGITS_FP32 ? 4 : 2)) return A3_EINVAL;
+  if ((p.M > 1 && p.row_stride < (uint64_t)p.vocab) || p.row_stride > (uint64_t)1 << 31) return A3_EINVAL;
+  const LogprobArgs a{p.logits, (long long)p.row_stride, p.M, p.vocab, p.targets, p.n_top, p.logprob_out, p.entropy_out, p.top_ids_out, p.top_logprobs_out, h->dev_status};
   cudaStream_t st = (cudaStream_t)stream;
   ProfScope prof(h, A3_K_FIRST_TOKEN, st);
-  return type == A3_LOGITS_FP32 ? logprobs_launch<float>(h, a, st) : type == A3_LOGITS_BF16 ? logprobs_launch<bf16>(h, a, st)
-                                                                                            : logprobs_launch<__half>(h, a, st);
+  return p.type == A3_LOGITS_FP32 ? logprobs_launch<float>(h, a, st) : p.type == A3_LOGITS_BF16 ? logprobs_launch<bf16>(h, a, st)
+                                                                                                : logprobs_launch<__half>(h, a, st);
 }

@@ -162,37 +162,36 @@ int paged_cache_check(const a3_handle* h, const a3_paged_cache* c) {
 
 using namespace a3;
 
-extern "C" int a3_paged_append(const a3_handle* h, const a3_paged_cache* cache, const int32_t* page_table, int n_seqs, int max_pages,
-                               const int32_t* row_seq, const int32_t* row_slot, const int32_t* row_pos, int rotate, const void* q_rows,
-                               size_t q_stride, const void* k_rows, size_t k_stride, const void* v_rows, size_t v_stride, int M, void* q_out,
-                               size_t q_out_stride, a3_stream stream) {
-  if (!h || !cache || M < 0 || n_seqs < 0 || max_pages < 0) return A3_EINVAL;
+extern "C" int a3_paged_append(const a3_handle* h, const a3_paged_cache* cache, const a3_paged_rows* rows, a3_stream stream) {
+  if (!h || !cache || !rows) return A3_EINVAL;
+  const a3_paged_rows& p = *rows;
+  if (p.M < 0 || p.n_seqs < 0 || p.max_pages < 0) return A3_EINVAL;
   A3_TRY(paged_cache_check(h, cache));
-  if (M == 0) return A3_OK;
-  if (!page_table || !row_seq || !row_slot || !k_rows || !v_rows || !q_rows != !q_out) return A3_EINVAL;
-  if (((uintptr_t)q_rows | (uintptr_t)k_rows | (uintptr_t)v_rows | (uintptr_t)q_out) & 15) return A3_EINVAL;
+  if (p.M == 0) return A3_OK;
+  if (!p.page_table || !p.row_seq || !p.row_slot || !p.k_rows || !p.v_rows || !p.q_rows != !p.q_out) return A3_EINVAL;
+  if (((uintptr_t)p.q_rows | (uintptr_t)p.k_rows | (uintptr_t)p.v_rows | (uintptr_t)p.q_out) & 15) return A3_EINVAL;
   const a3_model_desc& m = h->m;
-  const size_t qd = (size_t)m.n_q_heads * m.head_dim, kvd = (size_t)m.n_kv_heads * m.head_dim;
-  if (k_stride < kvd || v_stride < kvd || (q_rows && (q_stride < qd || q_out_stride < qd))) return A3_EINVAL;
-  if ((k_stride | v_stride | (q_rows ? q_stride | q_out_stride : 0)) % 8) return A3_EINVAL;
-  const size_t most = (size_t)1 << 40;  // elements between rows: offsets stay inside 63 bits
-  if (k_stride > most || v_stride > most || (q_rows && (q_stride > most || q_out_stride > most))) return A3_EINVAL;
+  const uint64_t qd = (uint64_t)m.n_q_heads * m.head_dim, kvd = (uint64_t)m.n_kv_heads * m.head_dim;
+  if (p.k_stride < kvd || p.v_stride < kvd || (p.q_rows && (p.q_stride < qd || p.q_out_stride < qd))) return A3_EINVAL;
+  if ((p.k_stride | p.v_stride | (p.q_rows ? p.q_stride | p.q_out_stride : 0)) % 8) return A3_EINVAL;
+  const uint64_t most = (uint64_t)1 << 31;  // elements between rows: offsets stay inside 63 bits
+  if (p.k_stride > most || p.v_stride > most || (p.q_rows && (p.q_stride > most || p.q_out_stride > most))) return A3_EINVAL;
   AppendArgs a{};
   a.k_pages = (char*)cache->k_pages, a.v_pages = (char*)cache->v_pages;
   a.page_stride = (long long)cache->page_stride, a.n_pages = cache->n_pages, a.page_size = cache->page_size;
   a.k_scale = cache->k_scale, a.v_scale = cache->v_scale;
-  a.table = page_table, a.row_seq = row_seq, a.row_slot = row_slot, a.row_pos = row_pos;
-  a.n_seqs = n_seqs, a.max_pages = max_pages;
-  a.q = (const bf16*)q_rows, a.k = (const bf16*)k_rows, a.v = (const bf16*)v_rows;
-  a.q_stride = (long long)q_stride, a.k_stride = (long long)k_stride, a.v_stride = (long long)v_stride, a.q_out_stride = (long long)q_out_stride;
-  a.q_out = (bf16*)q_out;
-  a.M = M, a.q_heads = q_rows ? m.n_q_heads : 0, a.kv_heads = m.n_kv_heads;
-  a.tab = h->rope_tab, a.max_pos = m.max_positions, a.rotate = rotate != 0, a.status = h->dev_status;
+  a.table = p.page_table, a.row_seq = p.row_seq, a.row_slot = p.row_slot, a.row_pos = p.row_pos;
+  a.n_seqs = p.n_seqs, a.max_pages = p.max_pages;
+  a.q = (const bf16*)p.q_rows, a.k = (const bf16*)p.k_rows, a.v = (const bf16*)p.v_rows;
+  a.q_stride = (long long)p.q_stride, a.k_stride = (long long)p.k_stride, a.v_stride = (long long)p.v_stride, a.q_out_stride = (long long)p.q_out_stride;
+  a.q_out = (bf16*)p.q_out;
+  a.M = p.M, a.q_heads = p.q_rows ? m.n_q_heads : 0, a.kv_heads = m.n_kv_heads;
+  a.tab = h->rope_tab, a.max_pos = m.max_positions, a.rotate = p.rotate != 0, a.status = h->dev_status;
   // one head for each thread as long as that fills the device, then four
   const int all = a.q_heads + 2 * a.kv_heads, uph = m.head_dim / 16;
-  const bool many = (unsigned long long)M * all * uph > (unsigned long long)h->sm_count * PA_ONE;
+  const bool many = (unsigned long long)p.M * all * uph > (unsigned long long)h->sm_count * PA_ONE;
   const int heads = many ? PA_HEADS : 1;
-  const unsigned long long need = ((unsigned long long)M * cdiv(all, heads) * uph + PA_THREADS - 1) / PA_THREADS;
+  const unsigned long long need = ((unsigned long long)p.M * cdiv(all, heads) * uph + PA_THREADS - 1) / PA_THREADS;
   const unsigned blocks = (unsigned)(need < (unsigned long long)h->sm_count * PA_MIN ? need : (unsigned long long)h->sm_count * PA_MIN);
   cudaStream_t st = (cudaStream_t)stream;
   ProfScope prof(h, A3_K_ROWS, st);

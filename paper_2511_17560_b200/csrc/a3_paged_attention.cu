@@ -28,6 +28,9 @@ namespace a3 {
 
 constexpr int PD_WARPS = 8;  // of a CTA, one per SM
 constexpr float LN2 = 0.693147180559945309f;
+// Tiles of a warp up to which one CTA may have a sequence alone: one sequence of 512 slots (32 query heads over 8, bf16) 7.0 us in one launch and
+// 9.1 in two, of 768 8.8 and 9.1, of 1 024 10.6 and 9.1; in 8 bits, where a tile is twice as many slots, of 1 024 8.1 and 9.8, of 2 048 12.7 and 9.8.
+constexpr int PD_ALONE = 5;
 constexpr int PD_LEAST = 2;  // tiles of a warp, before another part is begun
 constexpr float PD_SLACK = 8.f;  // see the running softmax
 
@@ -45,6 +48,7 @@ struct PagedAttnArgs {
   float* lse;
   int q_heads, kv_heads, group, groups;  // groups: CTAs' head units per KV head, of `unit` query heads at most
   int unit, parts;
+  bool by_seq;            // parts are sequences
   // workspace
   int4* meta;             // [parts]: what the join of part p does, see there
   float* part_o;          // [parts][units][2][unit][D]
@@ -141,17 +145,17 @@ paged_attention_kernel(const PagedAttnArgs a) {
   float* first_o = a.first_o + (long long)blockIdx.x * WARPS * a.unit * D;
   if (threadIdx.x < 2 * WARPS) s_info[threadIdx.x].seq = -1;
 
-  pdl_wait();
-  pdl_launch_dependents();
-  const float ks = F8 ? __ldcg(a.k_scale + kvh) : 1.f, vs = F8 ? __ldcg(a.v_scale + kvh) : 1.f;
-
-  // What a warp will want once it knows its place is sent for into L2 while the lengths are on their way: every thread of the device
-  // one line of the page table and one of the queries.
+  // What a warp will want once it knows its place is sent for into L2 before anything is known - a launch
+  // before this one may still be writing there -: every thread of the device one line of the page table and one of the queries.
   {
     const unsigned line = blockIdx.x * C::THREADS + threadIdx.x, per_seq = a.q_heads * (D / 64), s = line / per_seq;
     if (line < (unsigned long long)a.n_seqs * a.max_pages / 32) prefetch_l2(a.table + line * 32ull);
     if (s < (unsigned)a.n_seqs) prefetch_l2(a.q + s * a.q_stride + (line - s * per_seq) * 64);
   }
+
+  pdl_wait();
+  pdl_launch_dependents();
+  const float ks = F8 ? __ldcg(a.k_scale + kvh) : 1.f, vs = F8 ? __ldcg(a.v_scale + kvh) : 1.f;
 
   // ---- the line: every thread adds up the tiles of a stretch of sequences; each warp for itself or, where they are many, all together
   const long long cap = (long long)a.max_pages * a.page_size;
@@ -159,79 +163,90 @@ paged_attention_kernel(const PagedAttnArgs a) {
     const int n = __ldcg(a.lens + s);
     return n < 0 || n > cap ? 0 : n;
   };
-  const bool alone = a.n_seqs <= 256;
-  const int me = alone ? lane : threadIdx.x, per = (a.n_seqs + (alone ? 31 : C::THREADS - 1)) / (alone ? 32 : C::THREADS);
-  const int s0 = min(a.n_seqs, me * per), s1 = min(a.n_seqs, s0 + per);
-  unsigned mine = 0;
-  int n0 = 0;  // the first of them
-  for (int s = s0; s < s1; ++s) {
-    const int n = length(s);
-    if (s == s0) n0 = n;
-    mine += (n + KT - 1) / KT;
-  }
-  unsigned upto = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const unsigned t = __shfl_up_sync(0xffffffffu, upto, o);
-    if (lane >= o) upto += t;
-  }
-  unsigned total = __shfl_sync(0xffffffffu, upto, 31), before = upto - mine;
-  if (!alone) {
-    if (lane == 31) s_scan[warp] = upto;
-    __syncthreads();
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < WARPS; ++w) {
-      if (w < warp) before += s_scan[w];
-      total += s_scan[w];
+  auto nothing = [&](int s) {  // a sequence with nothing to attend to: no weight anywhere
+    if (__ldcg(a.lens + s) != 0 && hu == 0) atomicOr(a.status, A3_DEV_BAD_POSITION);
+    for (int h = h0; h < h0 + hn; ++h) {
+      uint4* o = reinterpret_cast<uint4*>(a.out + ((long long)s * a.q_heads + h) * D);
+      for (int i = 0; i < D / 8; ++i) o[i] = make_uint4(0, 0, 0, 0);
+      if (a.lse) a.lse[(long long)s * a.q_heads + h] = -INFINITY;
     }
-  }
-  if (part == 0 && (!alone || warp == 0)) {  // sequences with nothing to attend to: no weight anywhere
-    for (int s = s0; s < s1; ++s) {
-      if (length(s) > 0) continue;
-      if (__ldcg(a.lens + s) != 0 && hu == 0) atomicOr(a.status, A3_DEV_BAD_POSITION);
-      for (int h = h0; h < h0 + hn; ++h) {
-        uint4* o = reinterpret_cast<uint4*>(a.out + ((long long)s * a.q_heads + h) * D);
-        for (int i = 0; i < D / 8; ++i) o[i] = make_uint4(0, 0, 0, 0);
-        if (a.lse) a.lse[(long long)s * a.q_heads + h] = -INFINITY;
-      }
-    }
-  }
-  const int active = (int)min((total + PD_LEAST * WARPS - 1) / (PD_LEAST * WARPS), (unsigned)a.parts);
-  if (part >= active) {
-    if (hu == 0 && threadIdx.x == 0) a.meta[part] = make_int4(0, 0, 0, 0);
-    return;
-  }
-  const Parts parts(total, active);
-  const unsigned c0 = parts.begin(part), c1 = parts.begin(part + 1);
+  };
+  Parts parts(0, 1);
+  unsigned c0 = 0, c1, w0;  // this part's tiles of the line; the first of this warp's
   auto warp_begin = [&](int w) { return c0 + (unsigned)((unsigned long long)(c1 - c0) * w / WARPS); };
-  const unsigned w0 = warp_begin(warp);
-  const int count = (int)(warp_begin(warp + 1) - w0);
   // the sequence that this warp's stretch begins in: its number, its length, its first tile
   int seq0 = 0, len0 = 0;
   unsigned first0 = 0;
-  if (alone) {
-    for (int s = s0; s < s1; ++s) {
-      const int n = s == s0 ? n0 : length(s);
-      const unsigned tiles = (n + KT - 1) / KT;
-      if (w0 >= before && w0 < before + tiles) seq0 = s, len0 = n, first0 = before;
-      before += tiles;
+  if (a.by_seq) {  // a CTA for each sequence and head unit: a line of its own
+    seq0 = part, len0 = length(part), c1 = (len0 + KT - 1) / KT;
+    if (len0 == 0) {
+      if (threadIdx.x == 0) nothing(part);
+      return;
     }
-    const int who = __ffs(__ballot_sync(0xffffffffu, len0 > 0)) - 1;  // none where the stretch is empty and at the line's end
-    seq0 = __shfl_sync(0xffffffffu, seq0, who & 31), len0 = __shfl_sync(0xffffffffu, len0, who & 31), first0 = __shfl_sync(0xffffffffu, first0, who & 31);
+    w0 = warp_begin(warp);
   } else {
+    const bool alone = a.n_seqs <= 256;
+    const int me = alone ? lane : threadIdx.x, per = (a.n_seqs + (alone ? 31 : C::THREADS - 1)) / (alone ? 32 : C::THREADS);
+    const int s0 = min(a.n_seqs, me * per), s1 = min(a.n_seqs, s0 + per);
+    unsigned mine = 0;
+    int n0 = 0;  // the first of them
     for (int s = s0; s < s1; ++s) {
-      const int n = s == s0 ? n0 : length(s);
-      const unsigned tiles = (n + KT - 1) / KT;
-      for (int w = 0; w < WARPS; ++w) {
-        const unsigned b = warp_begin(w);
-        if (b >= before && b < before + tiles) s_warp_seq[w] = s, s_warp_first[w] = before, s_warp_len[w] = n;
-      }
-      before += tiles;
+      const int n = length(s);
+      if (s == s0) n0 = n;
+      mine += (n + KT - 1) / KT;
     }
-    __syncthreads();
-    seq0 = s_warp_seq[warp], len0 = s_warp_len[warp], first0 = s_warp_first[warp];
+    unsigned upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const unsigned t = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += t;
+    }
+    unsigned total = __shfl_sync(0xffffffffu, upto, 31), before = upto - mine;
+    if (!alone) {
+      if (lane == 31) s_scan[warp] = upto;
+      __syncthreads();
+      total = 0;
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) {
+        if (w < warp) before += s_scan[w];
+        total += s_scan[w];
+      }
+    }
+    if (part == 0 && (!alone || warp == 0))
+      for (int s = s0; s < s1; ++s)
+        if (length(s) == 0) nothing(s);
+    const int active = (int)min((total + PD_LEAST * WARPS - 1) / (PD_LEAST * WARPS), (unsigned)a.parts);
+    if (part >= active) {
+      if (hu == 0 && threadIdx.x == 0) a.meta[part] = make_int4(0, 0, 0, 0);
+      return;
+    }
+    parts = Parts(total, active);
+    c0 = parts.begin(part), c1 = parts.begin(part + 1);
+    w0 = warp_begin(warp);
+    if (alone) {
+      for (int s = s0; s < s1; ++s) {
+        const int n = s == s0 ? n0 : length(s);
+        const unsigned tiles = (n + KT - 1) / KT;
+        if (w0 >= before && w0 < before + tiles) seq0 = s, len0 = n, first0 = before;
+        before += tiles;
+      }
+      const int who = __ffs(__ballot_sync(0xffffffffu, len0 > 0)) - 1;  // none where the stretch is empty and at the line's end
+      seq0 = __shfl_sync(0xffffffffu, seq0, who & 31), len0 = __shfl_sync(0xffffffffu, len0, who & 31), first0 = __shfl_sync(0xffffffffu, first0, who & 31);
+    } else {
+      for (int s = s0; s < s1; ++s) {
+        const int n = s == s0 ? n0 : length(s);
+        const unsigned tiles = (n + KT - 1) / KT;
+        for (int w = 0; w < WARPS; ++w) {
+          const unsigned b = warp_begin(w);
+          if (b >= before && b < before + tiles) s_warp_seq[w] = s, s_warp_first[w] = before, s_warp_len[w] = n;
+        }
+        before += tiles;
+      }
+      __syncthreads();
+      seq0 = s_warp_seq[warp], len0 = s_warp_len[warp], first0 = s_warp_first[warp];
+    }
   }
+  const int count = (int)(warp_begin(warp + 1) - w0);
   __syncthreads();  // s_info
 
   // ---- this warp's stretch
@@ -263,7 +278,11 @@ paged_attention_kernel(const PagedAttnArgs a) {
     // Three steps of a tile, each in its own turn: its pages are looked up, three turns later its rows are copied, two turns after that it
     // is computed.  Pages and rows come by asynchronous copies, so that no turn waits for an access that it makes itself.
     int xs = seq0, xn = len0, xt = (int)(w0 - first0), xp = xt * KT / a.page_size, xe = xt * KT - xp * a.page_size;
-    int x_left = count, x_next = xs + 1 < a.n_seqs ? length(xs + 1) : 0;
+    int x_left = count, x_next = 0;
+    auto length_ahead = [&] {  // of the sequence behind this one, where the stretch goes on there or may
+      if (x_left > (xn + KT - 1) / KT - xt && xs + 1 < a.n_seqs) x_next = length(xs + 1);
+    };
+    length_ahead();
     auto look_up = [&](int j) {
       if (x_left <= 0) return;
       const int32_t* row = a.table + (long long)xs * a.max_pages;
@@ -284,7 +303,7 @@ paged_attention_kernel(const PagedAttnArgs a) {
         ++xs;
         xn = x_next;
         while (xn == 0) xn = length(++xs);
-        x_next = xs + 1 < a.n_seqs ? length(xs + 1) : 0;
+        length_ahead();
       } else if (WHOLE && (xe += KT) == a.page_size) {
         xe = 0;
         ++xp;
@@ -593,7 +612,7 @@ paged_attention_kernel(const PagedAttnArgs a) {
       }
     }
   }
-  if (hu == 0 && threadIdx.x == 0) {  // first0 and len0 are of the sequence that the part begins with
+  if (!a.by_seq && hu == 0 && threadIdx.x == 0) {  // first0 and len0 are of the sequence that the part begins with
     const int from = first0 < c0 ? parts.of(first0) : part, to = parts.of(first0 + (unsigned)(len0 + KT - 1) / KT - 1);
     a.meta[part] = make_int4(seq0, from, from == part - 1 ? to - from + 1 : 0, 0);
   }
@@ -757,13 +776,16 @@ static PagedPlan paged_plan(const a3_handle* h) {
 }
 
 template <int D, bool F8, int NT, bool WHOLE>
-static int paged_launch(const a3_handle* h, const PagedAttnArgs& a, int units, cudaStream_t st) {
+static int paged_launch(const a3_handle* h, PagedAttnArgs a, int units, cudaStream_t st) {
   static SmemAttrOnce once;
   using C = PagedCfg<D, F8, NT>;
+  // A CTA for each sequence and head unit needs no second launch; worth it where all of them run at once and none has many tiles, whatever the
+  // lengths turn out to be within the page table's width.
+  a.by_seq = (long long)a.n_seqs * units <= h->sm_count && (long long)a.max_pages * a.page_size <= PD_ALONE * C::WARPS * C::KT;
   A3_TRY(smem_attr_once(once, h->device, paged_attention_kernel<D, F8, NT, WHOLE>, C::SMEM));
-  A3_CUDA(launch_pdl(paged_attention_kernel<D, F8, NT, WHOLE>, dim3(a.parts * units), dim3(C::THREADS), C::SMEM, st, a));
+  A3_CUDA(launch_pdl(paged_attention_kernel<D, F8, NT, WHOLE>, dim3((a.by_seq ? a.n_seqs : a.parts) * units), dim3(C::THREADS), C::SMEM, st, a));
   A3_LAUNCHED();
-  if (a.parts == 1) return A3_OK;  // every sequence ends in the part that it begins in
+  if (a.by_seq || a.parts == 1) return A3_OK;  // every sequence ends in the part that it begins in
   A3_CUDA(launch_pdl(paged_join_kernel<D>, dim3(a.parts - 1, units, a.unit), dim3(32 * PJ_WARPS), a.parts * sizeof(float), st, a));
   return launched();
 }
@@ -774,35 +796,35 @@ using namespace a3;
 
 extern "C" size_t a3_paged_attention_workspace_bytes(const a3_handle* h) { return h ? paged_plan(h).bytes : 0; }
 
-extern "C" int a3_paged_attention(const a3_handle* h, const a3_paged_cache* cache, const int32_t* page_table, int n_seqs, int max_pages,
-                                  const int32_t* cache_len, const void* q_rows, size_t q_stride, float scale, void* out, float* lse_out,
-                                  void* ws, size_t ws_bytes, a3_stream stream) {
-  if (!h || !cache || n_seqs < 0 || max_pages < 0 || !isfinite(scale)) return A3_EINVAL;
+extern "C" int a3_paged_attention(const a3_handle* h, const a3_paged_cache* cache, const a3_paged_queries* queries, a3_stream stream) {
+  if (!h || !cache || !queries) return A3_EINVAL;
+  const a3_paged_queries& p = *queries;
+  if (p.n_seqs < 0 || p.max_pages < 0 || !isfinite(p.scale)) return A3_EINVAL;
   A3_TRY(paged_cache_check(h, cache));
   // slots of a sequence and tiles of all sequences (16 slots at least) are counted in 32 bits
-  const unsigned long long slots = (unsigned long long)max_pages * cache->page_size;
-  if (slots > 0x7fff0000ull || (n_seqs > 0 && slots > (1ull << 34) / n_seqs)) return A3_ETOOLARGE;
-  if (n_seqs == 0) return A3_OK;
-  if ((!page_table && max_pages > 0) || !cache_len || !q_rows || !out || !ws) return A3_EINVAL;
-  if (((uintptr_t)q_rows | (uintptr_t)out) & 15 || (uintptr_t)ws & 255) return A3_EINVAL;
+  const unsigned long long slots = (unsigned long long)p.max_pages * cache->page_size;
+  if (slots > 0x7fff0000ull || (p.n_seqs > 0 && slots > (1ull << 34) / p.n_seqs)) return A3_ETOOLARGE;
+  if (p.n_seqs == 0) return A3_OK;
+  if ((!p.page_table && p.max_pages > 0) || !p.cache_len || !p.q_rows || !p.out || !p.ws) return A3_EINVAL;
+  if (((uintptr_t)p.q_rows | (uintptr_t)p.out) & 15 || (uintptr_t)p.ws & 255) return A3_EINVAL;
   const a3_model_desc& m = h->m;
-  if (q_stride < (size_t)m.n_q_heads * m.head_dim || q_stride % 8 || q_stride > (size_t)1 << 40) return A3_EINVAL;
+  if (p.q_stride < (uint64_t)m.n_q_heads * m.head_dim || p.q_stride % 8 || p.q_stride > (uint64_t)1 << 31) return A3_EINVAL;
   const PagedPlan plan = paged_plan(h);
-  if (ws_bytes < plan.bytes) return A3_EWORKSPACE;
+  if (p.ws_bytes < plan.bytes) return A3_EWORKSPACE;
   PagedAttnArgs a{};
   a.k_pages = (const char*)cache->k_pages, a.v_pages = (const char*)cache->v_pages;
   a.page_stride = (long long)cache->page_stride, a.n_pages = cache->n_pages, a.page_size = cache->page_size;
   a.k_scale = cache->k_scale, a.v_scale = cache->v_scale;
-  a.table = page_table, a.lens = cache_len, a.n_seqs = n_seqs, a.max_pages = max_pages;
-  a.q = (const bf16*)q_rows, a.q_stride = (long long)q_stride;
-  a.scale_log2 = scale * 1.44269504088896341f;
-  a.out = (bf16*)out, a.lse = lse_out;
+  a.table = p.page_table, a.lens = p.cache_len, a.n_seqs = p.n_seqs, a.max_pages = p.max_pages;
+  a.q = (const bf16*)p.q_rows, a.q_stride = (long long)p.q_stride;
+  a.scale_log2 = p.scale * 1.44269504088896341f;
+  a.out = (bf16*)p.out, a.lse = p.lse_out;
   a.q_heads = m.n_q_heads, a.kv_heads = m.n_kv_heads, a.group = m.n_q_heads / m.n_kv_heads;
   a.unit = plan.unit, a.groups = plan.groups, a.parts = plan.parts;
-  a.meta = (int4*)ws;
-  a.part_ml = (float2*)((char*)ws + plan.meta);
-  a.part_o = (float*)((char*)ws + plan.meta + plan.ml);
-  a.first_o = (float*)((char*)ws + plan.meta + plan.ml + plan.o);
+  a.meta = (int4*)p.ws;
+  a.part_ml = (float2*)((char*)p.ws + plan.meta);
+  a.part_o = (float*)((char*)p.ws + plan.meta + plan.ml);
+  a.first_o = (float*)((char*)p.ws + plan.meta + plan.ml + plan.o);
   a.status = h->dev_status;
   cudaStream_t st = (cudaStream_t)stream;
   const int units = m.n_kv_heads * plan.groups;

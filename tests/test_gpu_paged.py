@@ -380,24 +380,31 @@ def test_refusals_of_the_library(a3):
     nbytes = lib.a3_paged_attention_workspace_bytes(eng._h)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=DEV)
     p = lambda t: t.data_ptr()  # noqa: E731
-    good = dict(h=eng._h, c=C.byref(cache.desc), t=p(table), n=1, w=1, len=p(one), q=p(q), qs=hq * d, scale=0.1, o=p(o), lse=None, ws=p(ws), b=nbytes, st=0)
-    attend = lambda **kw: lib.a3_paged_attention(*{**good, **kw}.values())  # noqa: E731
-    assert attend() == 0
+    whole = lambda kw: [0 if v is None else v for v in kw.values()]  # noqa: E731
+    good = dict(t=p(table), len=p(one), q=p(q), o=p(o), lse=None, ws=p(ws), b=nbytes, qs=hq * d, n=1, w=1, scale=0.1, r=0)
+    attend = lambda h=eng._h, c=C.addressof(cache.desc), **kw: lib.a3_paged_attention(h, c, a3.PAGED_QUERIES.pack(*whole({**good, **kw})), 0)  # noqa: E731
+    assert attend() == 0 and lib.a3_paged_attention(eng._h, cache._ref, None, 0) == -1 and lib.a3_paged_append(eng._h, cache._ref, None, 0) == -1
     a3.launch_count(reset=True)
-    desc = lambda **kw: C.byref(a3.PagedCacheDesc(*{**{f: getattr(cache.desc, f) for f, _ in a3.PagedCacheDesc._fields_}, **kw}.values()))  # noqa: E731
+    kept = []
+
+    def desc(**kw):
+        kept.append(a3.PagedCacheDesc(*{**{f: getattr(cache.desc, f) for f, _ in a3.PagedCacheDesc._fields_}, **kw}.values()))
+        return C.addressof(kept[-1])
+
     bad_caches = [dict(k_pages=None), dict(v_pages=p(vp) + 2), dict(n_pages=0), dict(page_size=0), dict(page_stride=16 * hkv * d * 2 - 16),
                   dict(page_stride=16 * hkv * d * 2 + 8), dict(type=1), dict(page_stride=1 << 62)]
     for kw in [dict(h=None), dict(c=None), dict(t=None), dict(n=-1), dict(w=-1), dict(len=None), dict(q=None), dict(q=p(q) + 2), dict(qs=hq * d - 8),
-               dict(qs=hq * d + 4), dict(scale=math.inf), dict(scale=math.nan), dict(o=None), dict(o=p(o) + 8), dict(ws=None), dict(ws=p(ws) + 16)]:
+               dict(qs=hq * d + 4), dict(qs=1 << 32), dict(scale=math.inf), dict(scale=math.nan), dict(o=None), dict(o=p(o) + 8), dict(ws=None), dict(ws=p(ws) + 16)]:
         assert attend(**kw) == -1, kw
     for kw in bad_caches:
         assert attend(c=desc(**kw)) == -1, kw
     assert attend(c=desc(type=2)) == -2 and attend(b=nbytes - 1) == -3 and attend(n=0) == 0
-    good_a = dict(h=eng._h, c=C.byref(cache.desc), t=p(table), n=1, w=1, seq=p(zero), slot=p(zero), pos=None, rot=1, q=p(q), qs=hq * d, k=p(k),
-                  ks=hkv * d, v=p(v), vs=hkv * d, M=1, o=p(o), os=hq * d, st=0)
-    append = lambda **kw: lib.a3_paged_append(*{**good_a, **kw}.values())  # noqa: E731
+    assert attend(w=1 << 27) == -6 and attend(n=1 << 10, w=(1 << 20) + 1) == -6
+    good_a = dict(t=p(table), seq=p(zero), slot=p(zero), pos=None, q=p(q), k=p(k), v=p(v), o=p(o), qs=hq * d, ks=hkv * d, vs=hkv * d, os=hq * d,
+                  n=1, w=1, M=1, rot=1)
+    append = lambda h=eng._h, c=C.addressof(cache.desc), **kw: lib.a3_paged_append(h, c, a3.PAGED_ROWS.pack(*whole({**good_a, **kw})), 0)  # noqa: E731
     for kw in [dict(h=None), dict(c=None), dict(t=None), dict(n=-1), dict(w=-1), dict(seq=None), dict(slot=None), dict(k=None), dict(v=None),
-               dict(q=None), dict(o=None), dict(M=-1), dict(k=p(k) + 2), dict(ks=hkv * d - 8), dict(vs=hkv * d + 1), dict(qs=8), dict(os=hq * d + 4)]:
+               dict(q=None), dict(o=None), dict(M=-1), dict(k=p(k) + 2), dict(ks=hkv * d - 8), dict(vs=hkv * d + 1), dict(qs=8), dict(os=hq * d + 4), dict(ks=1 << 32)]:
         assert append(**kw) == -1, kw
     for kw in bad_caches:
         assert append(c=desc(**kw)) == -1, kw

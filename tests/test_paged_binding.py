@@ -22,11 +22,17 @@ class Recorder:
     def a3_paged_attention_workspace_bytes(self, h):
         return 512
 
-    def _note(self, *args):
-        self.calls.append(args)
+    def a3_paged_append(self, h, cache, rows, stream):
+        self.calls.append(a3.PAGED_ROWS.unpack(rows))
         return 0
 
-    a3_paged_append = a3_paged_attention = a3_token_logprobs = _note
+    def a3_paged_attention(self, h, cache, queries, stream):
+        self.calls.append(a3.PAGED_QUERIES.unpack(queries))
+        return 0
+
+    def a3_token_logprobs(self, h, rows, stream):
+        self.calls.append(a3.LOGIT_ROWS.unpack(rows))
+        return 0
 
 
 @pytest.fixture
@@ -76,8 +82,12 @@ def test_append_arguments(eng):
     out = eng.paged_append(cache, table, seq, seq, k, v, q_rows=q)
     args = eng.calls[-1]
     assert out.shape == (5, 4, 64) and out.is_contiguous()
-    assert args[3:5] == (2, 2) and args[7:9] == (None, 1) and args[10] == 512 and args[12] == 512 and args[14:16] == (512, 5) and args[17] == 256
-    assert eng.paged_append(cache, table, seq, seq, k, v, rotate=False) is None and eng.calls[-1][8:11] == (0, None, 0)
+    assert args == (table.data_ptr(), seq.data_ptr(), seq.data_ptr(), 0, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), 512, 512, 512, 256,
+                    2, 2, 5, 1)
+    assert eng.paged_append(cache, table, seq, seq, k, v, rotate=False) is None
+    assert eng.calls[-1][4] == eng.calls[-1][7] == 0 and eng.calls[-1][15] == 0
+    eng.paged_append(cache, table, seq[:1], seq[:1], k[:1], v[:1], q_rows=q[:1])
+    assert eng.calls[-1][8:12] == (256, 128, 128, 256) and eng.calls[-1][14] == 1
     calls = len(eng.calls)
     flat = torch.zeros((5, 64, 2), dtype=torch.bfloat16).transpose(1, 2)
     for kw in [dict(page_table=table.long()), dict(page_table=table[0]), dict(page_table=torch.zeros((2, 4), dtype=torch.int32)[:, ::2]), dict(row_seq=seq[:4]), dict(row_seq=seq.long()), dict(row_slot=seq[::2]),
@@ -94,10 +104,11 @@ def test_attention_arguments(eng):
     out, lse = eng.paged_attention(cache, table, lens, q, want_lse=True)
     args = eng.calls[-1]
     assert out.shape == (3, 4, 64) and lse.shape == (3, 4) and lse.dtype == torch.float32
-    assert args[3:5] == (3, 2) and args[7] == 384 and args[8] == 64 ** -0.5 and args[12] == 512
+    assert args[:5] == (table.data_ptr(), lens.data_ptr(), q.data_ptr(), out.data_ptr(), lse.data_ptr()) and args[6:10] == (512, 384, 3, 2)
+    assert abs(args[10] - 64 ** -0.5) < 1e-8
     given = torch.empty((3, 4, 64), dtype=torch.bfloat16)
     out, lse = eng.paged_attention(cache, table, lens, q, scale=0.5, out=given)
-    assert out is given and lse is None and eng.calls[-1][8] == 0.5 and eng.calls[-1][10] is None
+    assert out is given and lse is None and eng.calls[-1][10] == 0.5 and eng.calls[-1][4] == 0
     calls = len(eng.calls)
     for kw in [dict(cache_len=lens[:2]), dict(cache_len=lens.long()), dict(cache_len=lens[None]), dict(page_table=table.long()), dict(page_table=table[:2]),
                dict(q_rows=q.float()), dict(q_rows=q[:2]), dict(q_rows=q[:, :2]), dict(q_rows=q[..., :32]), dict(out=given[:2]), dict(out=given.float()),
@@ -110,28 +121,43 @@ def test_logprob_arguments(eng):
     x = torch.zeros((3, 80), dtype=torch.bfloat16)
     logprob, entropy, ids, lps = eng.token_logprobs(x[:, 1:70], i32(0, 1, -1), 4)
     assert logprob.shape == entropy.shape == (3,) and ids.shape == lps.shape == (3, 4) and ids.dtype == torch.int32
-    assert eng.calls[-1][2:6] == (1, 80, 3, 69) and eng.calls[-1][7] == 4
+    assert eng.calls[-1][6:] == (80, 1, 3, 69, 4)
     logprob, entropy, ids, lps = eng.token_logprobs(x)
-    assert logprob is ids is lps is None and eng.calls[-1][6:9] == (None, 0, None)
+    assert logprob is ids is lps is None and eng.calls[-1][1:3] == (0, 0) and eng.calls[-1][4:6] == (0, 0) and eng.calls[-1][10] == 0
     calls = len(eng.calls)
     for args in [(x[0],), (x.double(),), (x.t(),), (x[:, ::2],), (x[:, :0],), (x, i32(0, 1)), (x, i32(0, 1, 2).long()), (x, i32(0, 1, 2)[None])]:
         refused(eng.token_logprobs, *args)
     assert len(eng.calls) == calls
 
 
-def test_cache_struct_matches_the_header(tmp_path):
+def test_structs_match_the_header(tmp_path):
+    """The packed forms have the header's size and order: each field's place as the C compiler sees it."""
+    fields = {"a3_paged_rows": ("page_table row_seq row_slot row_pos q_rows k_rows v_rows q_out q_stride k_stride v_stride q_out_stride n_seqs max_pages M "
+                                "rotate", a3.PAGED_ROWS),
+              "a3_paged_queries": ("page_table cache_len q_rows out lse_out ws ws_bytes q_stride n_seqs max_pages scale reserved", a3.PAGED_QUERIES),
+              "a3_logit_rows": ("logits targets logprob_out entropy_out top_ids_out top_logprobs_out row_stride type M vocab n_top", a3.LOGIT_ROWS)}
     lines = ['printf("%zu\\n", sizeof(a3_paged_cache));'] + [f'printf("%zu\\n", offsetof(a3_paged_cache, {f}));' for f, _ in a3.PagedCacheDesc._fields_]
+    want = [ctypes.sizeof(a3.PagedCacheDesc)] + [getattr(a3.PagedCacheDesc, f).offset for f, _ in a3.PagedCacheDesc._fields_]
+    for name, (names, packed) in fields.items():
+        lines += [f'printf("%zu\\n", sizeof({name}));'] + [f'printf("%zu\\n", offsetof({name}, {f}));' for f in names.split()]
+        # the place of a field is where the only byte that is not zero lies
+        want.append(packed.size)
+        for i in range(len(names.split())):
+            values = [0] * len(names.split())
+            values[i] = 1
+            data = packed.pack(*values)
+            at = next(k for k, b in enumerate(data) if b)
+            want.append(at // 4 * 4)
     src, exe = tmp_path / "layout.c", tmp_path / "layout"
     src.write_text('#include <stdio.h>\n#include <stddef.h>\n#include "a3.h"\nint main(void) {\n' + "\n".join(lines) + "\nreturn 0; }\n")
     inc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include")
     subprocess.run(["gcc", "-std=c99", "-I", inc, str(src), "-o", str(exe)], check=True)
-    got = [int(s) for s in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split()]
-    assert got == [ctypes.sizeof(a3.PagedCacheDesc)] + [getattr(a3.PagedCacheDesc, f).offset for f, _ in a3.PagedCacheDesc._fields_]
+    assert [int(s) for s in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split()] == want
 
 
 def test_null_handles():
     lib = a3._load()
     assert lib.a3_paged_attention_workspace_bytes(None) == 0
-    assert lib.a3_paged_append(None, None, None, 0, 0, None, None, None, 0, None, 0, None, 0, None, 0, 0, None, 0, None) == -1
-    assert lib.a3_paged_attention(None, None, None, 0, 0, None, None, 0, 1.0, None, None, None, 0, None) == -1
-    assert lib.a3_token_logprobs(None, None, 0, 0, 0, 1, None, 0, None, None, None, None, None) == -1
+    assert lib.a3_paged_append(None, None, None, None) == -1
+    assert lib.a3_paged_attention(None, None, None, None) == -1
+    assert lib.a3_token_logprobs(None, None, None) == -1
