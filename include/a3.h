@@ -416,14 +416,15 @@ typedef struct {
   const void* q_rows;        /* dev [n_seqs][Hq][D] bf16, 16-byte aligned */
   void* out;                 /* dev [n_seqs][Hq][D] bf16, 16-byte aligned */
   float* lse_out;            /* dev [n_seqs][Hq] natural-log row log-sum-exps of the scaled logits, or NULL */
-  void* ws;                  /* dev, 256-byte aligned, a3_paged_attention_workspace_bytes(h) bytes */
+  void* ws;                  /* dev, 256-byte aligned, a3_paged_attention_workspace_bytes bytes; not looked at where that is 0 */
   uint64_t ws_bytes;
   uint64_t q_stride;         /* elements between sequences, a multiple of 8 */
   int32_t n_seqs, max_pages;
   float scale;
   int32_t reserved;
 } a3_paged_queries;
-size_t a3_paged_attention_workspace_bytes(const a3_handle* h);
+/* For this cache, so many sequences and this width of the page table; 0 where few and short sequences need none. */
+size_t a3_paged_attention_workspace_bytes(const a3_handle* h, const a3_paged_cache* cache, int n_seqs, int max_pages);
 int a3_paged_attention(const a3_handle* h, const a3_paged_cache* cache, const a3_paged_queries* queries, a3_stream stream);
 
 /* Log probabilities of given tokens, entropies and the best alternatives, from rows of logits (a3_first_token's, or a projection of

@@ -131,7 +131,7 @@ def _load():
     lib.a3_first_token_workspace_bytes.restype = sz
     lib.a3_first_token.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, sz, vp]
     lib.a3_paged_append.argtypes = [vp, vp, C.c_char_p, vp]
-    lib.a3_paged_attention_workspace_bytes.argtypes = [vp]
+    lib.a3_paged_attention_workspace_bytes.argtypes = [vp, vp, i32, i32]
     lib.a3_paged_attention_workspace_bytes.restype = sz
     lib.a3_paged_attention.argtypes = [vp, vp, C.c_char_p, vp]
     lib.a3_token_logprobs.argtypes = [vp, C.c_char_p, vp]
@@ -511,10 +511,10 @@ class A3:
         elif not (out.dtype is torch.bfloat16 and out.shape == shape and out.is_contiguous() and out.device == dev):
             raise A3Error(-1, "a3_paged_attention: out")
         lse = q_rows.new_empty((n, Hq), dtype=torch.float32) if want_lse else None
-        nbytes = lib.a3_paged_attention_workspace_bytes(self._h)
-        ws = q_rows.new_empty(nbytes, dtype=torch.uint8)
+        nbytes = lib.a3_paged_attention_workspace_bytes(self._h, cache._ref, n, max_pages)
+        ws = q_rows.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
         status = lib.a3_paged_attention(self._h, cache._ref, PAGED_QUERIES.pack(
-            page_table.data_ptr(), cache_len.data_ptr(), q_rows.data_ptr(), out.data_ptr(), 0 if lse is None else lse.data_ptr(), ws.data_ptr(), nbytes,
+            page_table.data_ptr(), cache_len.data_ptr(), q_rows.data_ptr(), out.data_ptr(), 0 if lse is None else lse.data_ptr(), 0 if ws is None else ws.data_ptr(), nbytes,
             qr if n > 1 else Hq * D, n, max_pages, D ** -0.5 if scale is None else scale, 0), _stream())
         if status != A3_OK:
             raise A3Error(status, "a3_paged_attention")

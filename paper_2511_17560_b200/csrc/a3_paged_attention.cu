@@ -26,7 +26,8 @@
 
 namespace a3 {
 
-constexpr int PD_WARPS = 8;  // of a CTA, one per SM
+constexpr int PD_WARPS = 8;      // of a CTA, one per SM
+constexpr int PD_STAGE = 8192;   // bytes of a tile: keys in the lower half, values in the upper
 constexpr float LN2 = 0.693147180559945309f;
 // Tiles of a warp up to which one CTA may have a sequence alone: one sequence of 512 slots (32 query heads over 8, bf16) 7.0 us in one launch and
 // 9.1 in two, of 768 8.8 and 9.1, of 1 024 10.6 and 9.1; in 8 bits, where a tile is twice as many slots, of 1 024 8.1 and 9.8, of 2 048 12.7 and 9.8.
@@ -107,7 +108,7 @@ template <int D, bool F8, int NT>
 struct PagedCfg {
   static constexpr int ROWB = D * (F8 ? 1 : 2), CH = ROWB / 16, HN = 8 * NT;
   static constexpr int WARPS = PD_WARPS, THREADS = 32 * WARPS;
-  static constexpr int STAGE = 8192, HALF = STAGE / 2;  // bytes of a tile: keys in the lower half, values in the upper
+  static constexpr int STAGE = PD_STAGE, HALF = STAGE / 2;
   static constexpr int KT = HALF / ROWB, STAGES = 3, RING = STAGES * STAGE;
   static constexpr int SMEM = WARPS * RING;
   static_assert(HN * D * 4 <= RING, "a warp's last partial output lies in its ring");
@@ -775,13 +776,17 @@ static PagedPlan paged_plan(const a3_handle* h) {
   return p;
 }
 
+// A CTA for each sequence and head unit needs no second launch; worth it where all of them run at once and none has many tiles, whatever the
+// lengths turn out to be within the page table's width.
+static bool paged_alone(const a3_handle* h, const PagedPlan& plan, const a3_paged_cache* cache, int n_seqs, int max_pages) {
+  const int row = h->m.head_dim * (cache->type == A3_CACHE_E4M3 ? 1 : 2), tile = PD_STAGE / 2 / row;  // slots of a tile
+  return (long long)n_seqs * h->m.n_kv_heads * plan.groups <= h->sm_count && (long long)max_pages * cache->page_size <= (long long)PD_ALONE * PD_WARPS * tile;
+}
+
 template <int D, bool F8, int NT, bool WHOLE>
-static int paged_launch(const a3_handle* h, PagedAttnArgs a, int units, cudaStream_t st) {
+static int paged_launch(const a3_handle* h, const PagedAttnArgs& a, int units, cudaStream_t st) {
   static SmemAttrOnce once;
   using C = PagedCfg<D, F8, NT>;
-  // A CTA for each sequence and head unit needs no second launch; worth it where all of them run at once and none has many tiles, whatever the
-  // lengths turn out to be within the page table's width.
-  a.by_seq = (long long)a.n_seqs * units <= h->sm_count && (long long)a.max_pages * a.page_size <= PD_ALONE * C::WARPS * C::KT;
   A3_TRY(smem_attr_once(once, h->device, paged_attention_kernel<D, F8, NT, WHOLE>, C::SMEM));
   A3_CUDA(launch_pdl(paged_attention_kernel<D, F8, NT, WHOLE>, dim3((a.by_seq ? a.n_seqs : a.parts) * units), dim3(C::THREADS), C::SMEM, st, a));
   A3_LAUNCHED();
@@ -794,7 +799,11 @@ static int paged_launch(const a3_handle* h, PagedAttnArgs a, int units, cudaStre
 
 using namespace a3;
 
-extern "C" size_t a3_paged_attention_workspace_bytes(const a3_handle* h) { return h ? paged_plan(h).bytes : 0; }
+extern "C" size_t a3_paged_attention_workspace_bytes(const a3_handle* h, const a3_paged_cache* cache, int n_seqs, int max_pages) {
+  if (!h || !cache || n_seqs <= 0 || max_pages < 0) return 0;
+  const PagedPlan plan = paged_plan(h);
+  return paged_alone(h, plan, cache, n_seqs, max_pages) ? 0 : plan.bytes;
+}
 
 extern "C" int a3_paged_attention(const a3_handle* h, const a3_paged_cache* cache, const a3_paged_queries* queries, a3_stream stream) {
   if (!h || !cache || !queries) return A3_EINVAL;
@@ -805,12 +814,14 @@ extern "C" int a3_paged_attention(const a3_handle* h, const a3_paged_cache* cach
   const unsigned long long slots = (unsigned long long)p.max_pages * cache->page_size;
   if (slots > 0x7fff0000ull || (p.n_seqs > 0 && slots > (1ull << 34) / p.n_seqs)) return A3_ETOOLARGE;
   if (p.n_seqs == 0) return A3_OK;
-  if ((!p.page_table && p.max_pages > 0) || !p.cache_len || !p.q_rows || !p.out || !p.ws) return A3_EINVAL;
-  if (((uintptr_t)p.q_rows | (uintptr_t)p.out) & 15 || (uintptr_t)p.ws & 255) return A3_EINVAL;
+  if ((!p.page_table && p.max_pages > 0) || !p.cache_len || !p.q_rows || !p.out) return A3_EINVAL;
+  if (((uintptr_t)p.q_rows | (uintptr_t)p.out) & 15) return A3_EINVAL;
   const a3_model_desc& m = h->m;
   if (p.q_stride < (uint64_t)m.n_q_heads * m.head_dim || p.q_stride % 8 || p.q_stride > (uint64_t)1 << 31) return A3_EINVAL;
   const PagedPlan plan = paged_plan(h);
-  if (p.ws_bytes < plan.bytes) return A3_EWORKSPACE;
+  const bool alone = paged_alone(h, plan, cache, p.n_seqs, p.max_pages);
+  if (!alone && (!p.ws || (uintptr_t)p.ws & 255)) return A3_EINVAL;
+  if (!alone && p.ws_bytes < plan.bytes) return A3_EWORKSPACE;
   PagedAttnArgs a{};
   a.k_pages = (const char*)cache->k_pages, a.v_pages = (const char*)cache->v_pages;
   a.page_stride = (long long)cache->page_stride, a.n_pages = cache->n_pages, a.page_size = cache->page_size;
@@ -820,11 +831,13 @@ extern "C" int a3_paged_attention(const a3_handle* h, const a3_paged_cache* cach
   a.scale_log2 = p.scale * 1.44269504088896341f;
   a.out = (bf16*)p.out, a.lse = p.lse_out;
   a.q_heads = m.n_q_heads, a.kv_heads = m.n_kv_heads, a.group = m.n_q_heads / m.n_kv_heads;
-  a.unit = plan.unit, a.groups = plan.groups, a.parts = plan.parts;
-  a.meta = (int4*)p.ws;
-  a.part_ml = (float2*)((char*)p.ws + plan.meta);
-  a.part_o = (float*)((char*)p.ws + plan.meta + plan.ml);
-  a.first_o = (float*)((char*)p.ws + plan.meta + plan.ml + plan.o);
+  a.unit = plan.unit, a.groups = plan.groups, a.parts = plan.parts, a.by_seq = alone;
+  if (!alone) {
+    a.meta = (int4*)p.ws;
+    a.part_ml = (float2*)((char*)p.ws + plan.meta);
+    a.part_o = (float*)((char*)p.ws + plan.meta + plan.ml);
+    a.first_o = (float*)((char*)p.ws + plan.meta + plan.ml + plan.o);
+  }
   a.status = h->dev_status;
   cudaStream_t st = (cudaStream_t)stream;
   const int units = m.n_kv_heads * plan.groups;

@@ -376,14 +376,17 @@ def test_refusals_of_the_library(a3):
     kp, vp, _, _ = make_pool(g, 4, 16, hkv, d, False)
     cache, lib = a3.PagedCache(kp, vp), a3._load()
     q, k, v, o = randn(g, 1, hq, d), randn(g, 1, hkv, d), randn(g, 1, hkv, d), randn(g, 1, hq, d)
-    table, one, zero = ints([[0]]), ints([1]), ints([0])
-    nbytes = lib.a3_paged_attention_workspace_bytes(eng._h)
+    one, zero = ints([1]), ints([0])
+    wide = 1 << 12  # pages of a table that a sequence alone in a CTA is not meant for
+    table = torch.zeros((1, wide), dtype=torch.int32, device=DEV)
+    nbytes = lib.a3_paged_attention_workspace_bytes(eng._h, cache._ref, 1, wide)
+    assert nbytes > 0 and lib.a3_paged_attention_workspace_bytes(eng._h, cache._ref, 1, 1) == 0
     ws = torch.empty(nbytes, dtype=torch.uint8, device=DEV)
     p = lambda t: t.data_ptr()  # noqa: E731
     whole = lambda kw: [0 if v is None else v for v in kw.values()]  # noqa: E731
-    good = dict(t=p(table), len=p(one), q=p(q), o=p(o), lse=None, ws=p(ws), b=nbytes, qs=hq * d, n=1, w=1, scale=0.1, r=0)
+    good = dict(t=p(table), len=p(one), q=p(q), o=p(o), lse=None, ws=p(ws), b=nbytes, qs=hq * d, n=1, w=wide, scale=0.1, r=0)
     attend = lambda h=eng._h, c=C.addressof(cache.desc), **kw: lib.a3_paged_attention(h, c, a3.PAGED_QUERIES.pack(*whole({**good, **kw})), 0)  # noqa: E731
-    assert attend() == 0 and lib.a3_paged_attention(eng._h, cache._ref, None, 0) == -1 and lib.a3_paged_append(eng._h, cache._ref, None, 0) == -1
+    assert attend() == 0 and attend(w=1, ws=None, b=0) == 0 and lib.a3_paged_attention(eng._h, cache._ref, None, 0) == -1 and lib.a3_paged_append(eng._h, cache._ref, None, 0) == -1
     a3.launch_count(reset=True)
     kept = []
 

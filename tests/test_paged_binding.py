@@ -19,8 +19,8 @@ class Recorder:
     def __getattr__(self, name):
         return getattr(self._lib, name)
 
-    def a3_paged_attention_workspace_bytes(self, h):
-        return 512
+    def a3_paged_attention_workspace_bytes(self, h, cache, n_seqs, max_pages):
+        return 512 if n_seqs > 1 else 0
 
     def a3_paged_append(self, h, cache, rows, stream):
         self.calls.append(a3.PAGED_ROWS.unpack(rows))
@@ -109,6 +109,8 @@ def test_attention_arguments(eng):
     given = torch.empty((3, 4, 64), dtype=torch.bfloat16)
     out, lse = eng.paged_attention(cache, table, lens, q, scale=0.5, out=given)
     assert out is given and lse is None and eng.calls[-1][10] == 0.5 and eng.calls[-1][4] == 0
+    eng.paged_attention(cache, table[:1], lens[:1], q[:1])
+    assert eng.calls[-1][5:7] == (0, 0)  # no workspace where none is needed
     calls = len(eng.calls)
     for kw in [dict(cache_len=lens[:2]), dict(cache_len=lens.long()), dict(cache_len=lens[None]), dict(page_table=table.long()), dict(page_table=table[:2]),
                dict(q_rows=q.float()), dict(q_rows=q[:2]), dict(q_rows=q[:, :2]), dict(q_rows=q[..., :32]), dict(out=given[:2]), dict(out=given.float()),
@@ -157,7 +159,7 @@ def test_structs_match_the_header(tmp_path):
 
 def test_null_handles():
     lib = a3._load()
-    assert lib.a3_paged_attention_workspace_bytes(None) == 0
+    assert lib.a3_paged_attention_workspace_bytes(None, None, 1, 1) == 0
     assert lib.a3_paged_append(None, None, None, None) == -1
     assert lib.a3_paged_attention(None, None, None, None) == -1
     assert lib.a3_token_logprobs(None, None, None) == -1
