@@ -463,21 +463,25 @@ class A3:
             raise A3Error(-1, "a3_paged_append: row_pos")
         M, = rows
         kv_shape = (M, m.n_kv_heads, D)
+        if not (k_rows.shape == kv_shape and v_rows.shape == kv_shape and k_rows.dtype is v_rows.dtype is bf16 and k_rows.device == dev
+                and v_rows.device == dev):
+            raise A3Error(-1, "a3_paged_append: k_rows, v_rows: bf16 [M][Hkv][D] on the engine's device")
         kr, kh, ke = k_rows.stride()
         vr, vh, ve = v_rows.stride()
-        if not (k_rows.shape == kv_shape and v_rows.shape == kv_shape and k_rows.dtype is v_rows.dtype is bf16 and k_rows.device == dev
-                and v_rows.device == dev and (M == 0 or (ke == ve == 1 and (kh == vh == D or m.n_kv_heads == 1)))):
-            raise A3Error(-1, "a3_paged_append: k_rows, v_rows: bf16 [M][Hkv][D] on the engine's device, the heads of a row next to each other")
+        if M > 0 and not (ke == ve == 1 and (kh == vh == D or m.n_kv_heads == 1)):
+            raise A3Error(-1, "a3_paged_append: k_rows, v_rows: the heads of a row lie next to each other")
         q = out = qr = outr = 0
         if q_rows is not None:
             q_shape = (M, m.n_q_heads, D)
             if q_out is None:
                 q_out = q_rows.new_empty(q_shape)
+            if not (q_rows.shape == q_shape and q_out.shape == q_shape and q_rows.dtype is q_out.dtype is bf16 and q_rows.device == dev
+                    and q_out.device == dev):
+                raise A3Error(-1, "a3_paged_append: q_rows, q_out: bf16 [M][Hq][D] on the engine's device")
             qr, qh, qe = q_rows.stride()
             outr, oh, oe = q_out.stride()
-            if not (q_rows.shape == q_shape and q_out.shape == q_shape and q_rows.dtype is q_out.dtype is bf16 and q_rows.device == dev
-                    and q_out.device == dev and (M == 0 or (qe == oe == 1 and (qh == oh == D or m.n_q_heads == 1)))):
-                raise A3Error(-1, "a3_paged_append: q_rows, q_out: bf16 [M][Hq][D] on the engine's device, the heads of a row next to each other")
+            if M > 0 and not (qe == oe == 1 and (qh == oh == D or m.n_q_heads == 1)):
+                raise A3Error(-1, "a3_paged_append: q_rows, q_out: the heads of a row lie next to each other")
             q, out = q_rows.data_ptr(), q_out.data_ptr()
         elif q_out is not None:
             raise A3Error(-1, "a3_paged_append: q_out without q_rows")
@@ -502,10 +506,11 @@ class A3:
             raise A3Error(-1, "a3_paged_attention: cache of this model, and contiguous int32 page table and lengths, on the engine's device")
         n, max_pages = page_table.shape
         shape = (n, Hq, D)
+        if not (cache_len.shape[0] == n and q_rows.shape == shape and q_rows.dtype is torch.bfloat16 and q_rows.device == dev):
+            raise A3Error(-1, "a3_paged_attention: q_rows: bf16 [n_seqs][Hq][D] on the engine's device")
         qr, qh, qe = q_rows.stride()
-        if not (cache_len.shape[0] == n and q_rows.shape == shape and q_rows.dtype is torch.bfloat16 and q_rows.device == dev
-                and (n == 0 or (qe == 1 and (qh == D or Hq == 1)))):
-            raise A3Error(-1, "a3_paged_attention: q_rows: bf16 [n_seqs][Hq][D] on the engine's device, the heads of a row next to each other")
+        if n > 0 and not (qe == 1 and (qh == D or Hq == 1)):
+            raise A3Error(-1, "a3_paged_attention: q_rows: the heads of a row lie next to each other")
         if out is None:
             out = torch.empty_like(q_rows, memory_format=torch.contiguous_format)
         elif not (out.dtype is torch.bfloat16 and out.shape == shape and out.is_contiguous() and out.device == dev):

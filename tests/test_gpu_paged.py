@@ -365,6 +365,40 @@ def test_calls_on_another_stream(a3):
     assert all(torch.equal(want, o) for o in got)
 
 
+def test_attention_without_pages(a3):
+    """A page table of no columns: every sequence is padding."""
+    eng, g = engine(a3, "g4"), gen(20)
+    hq, hkv, d = SHAPES["g4"]
+    kp, vp, _, _ = make_pool(g, 1, 16, hkv, d, False)
+    for n in (1, 3, 400):
+        q = randn(g, n, hq, d)
+        out, lse = eng.paged_attention(a3.PagedCache(kp, vp), torch.empty((n, 0), dtype=torch.int32, device=DEV), ints([0] * n), q, want_lse=True)
+        assert (out == 0).all() and (lse == -math.inf).all() and eng.device_status() == 0
+    out, _ = eng.paged_attention(a3.PagedCache(kp, vp), torch.empty((0, 4), dtype=torch.int32, device=DEV), ints([]), q[:0])
+    assert out.shape == (0, hq, d)
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_attention_where_one_cta_or_many_have_a_sequence(a3, packed):
+    """The same sequences behind page tables of different widths: alone in a CTA each, and on the line of all CTAs."""
+    hq, hkv, d = SHAPES["g4"]
+    eng, g = engine(a3, "g4"), gen(21)
+    lens = [600, 1, 0, 17, 333]
+    narrow, n = make_table(g, lens, 16, width=40)
+    cache = a3.PagedCache(*make_pool(g, n, 16, hkv, d, packed))
+    q = randn(g, 5, hq, d, std=2.0)
+    lib = a3._load()
+    assert lib.a3_paged_attention_workspace_bytes(eng._h, cache._ref, 5, 40) == 0
+    wide = torch.full((5, 200), -3, dtype=torch.int32, device=DEV)
+    wide[:, :40] = narrow
+    assert lib.a3_paged_attention_workspace_bytes(eng._h, cache._ref, 5, 200) > 0
+    a3.launch_count(reset=True)
+    check_attention(a3, eng, cache, narrow, lens, q)
+    assert a3.launch_count() == 1
+    check_attention(a3, eng, cache, wide, lens, q)
+    assert a3.launch_count() == 3
+
+
 # ------------------------------------------------------------------ refusals
 
 

@@ -92,7 +92,7 @@ def test_append_arguments(eng):
     flat = torch.zeros((5, 64, 2), dtype=torch.bfloat16).transpose(1, 2)
     for kw in [dict(page_table=table.long()), dict(page_table=table[0]), dict(page_table=torch.zeros((2, 4), dtype=torch.int32)[:, ::2]), dict(row_seq=seq[:4]), dict(row_seq=seq.long()), dict(row_slot=seq[::2]),
                dict(row_pos=seq[:2]), dict(row_pos=seq.float()), dict(k_rows=k.float()), dict(k_rows=k[:4]), dict(k_rows=flat), dict(v_rows=q),
-               dict(v_rows=v[..., :32]), dict(q_rows=k), dict(q_rows=None, q_out=out), dict(q_out=out.float()), dict(q_out=out[:4]),
+               dict(v_rows=v[..., :32]), dict(q_rows=k), dict(k_rows=k.flatten(1)), dict(v_rows=v[0]), dict(q_rows=q.flatten(1)), dict(q_rows=q.transpose(1, 2).contiguous().transpose(1, 2)), dict(q_rows=None, q_out=out), dict(q_out=out.float()), dict(q_out=out[:4]),
                dict(cache=a3.PagedCache(pages(heads=4), pages(heads=4))), dict(cache=a3.PagedCache(pages(d=128), pages(d=128)))]:
         refused(eng.paged_append, **{**dict(cache=cache, page_table=table, row_seq=seq, row_slot=seq, k_rows=k, v_rows=v, q_rows=q), **kw})
     assert len(eng.calls) == calls
@@ -113,7 +113,7 @@ def test_attention_arguments(eng):
     assert eng.calls[-1][5:7] == (0, 0)  # no workspace where none is needed
     calls = len(eng.calls)
     for kw in [dict(cache_len=lens[:2]), dict(cache_len=lens.long()), dict(cache_len=lens[None]), dict(page_table=table.long()), dict(page_table=table[:2]),
-               dict(q_rows=q.float()), dict(q_rows=q[:2]), dict(q_rows=q[:, :2]), dict(q_rows=q[..., :32]), dict(out=given[:2]), dict(out=given.float()),
+               dict(q_rows=q.float()), dict(q_rows=q.flatten(1)), dict(q_rows=q[:2]), dict(q_rows=q[:, :2]), dict(q_rows=q[..., :32]), dict(out=given[:2]), dict(out=given.float()),
                dict(cache=a3.PagedCache(pages(heads=1), pages(heads=1)))]:
         refused(eng.paged_attention, **{**dict(cache=cache, page_table=table, cache_len=lens, q_rows=q), **kw})
     assert len(eng.calls) == calls
