@@ -32,6 +32,9 @@ constexpr float LN2 = 0.693147180559945309f;
 // Tiles of a warp up to which one CTA may have a sequence alone: one sequence of 512 slots (32 query heads over 8, bf16) 7.0 us in one launch and
 // 9.1 in two, of 768 8.8 and 9.1, of 1 024 10.6 and 9.1; in 8 bits, where a tile is twice as many slots, of 1 024 8.1 and 9.8, of 2 048 12.7 and 9.8.
 constexpr int PD_ALONE = 5;
+// From so many tiles for each warp on, one tile in PD_LATE goes to late parts: 128 sequences of up to 8 191 slots (213 tiles a warp) 321 -> 307 us,
+// 32 of them (57) 93.3 -> 91.1, 32 of 28 heads over 4 (40) 70.3 -> 71.8.
+constexpr int PD_MANY = 48, PD_LATE = 10;
 constexpr int PD_LEAST = 2;  // tiles of a warp, before another part is begun
 constexpr float PD_SLACK = 8.f;  // see the running softmax
 
@@ -48,7 +51,8 @@ struct PagedAttnArgs {
   bf16* out;
   float* lse;
   int q_heads, kv_heads, group, groups;  // groups: CTAs' head units per KV head, of `unit` query heads at most
-  int unit, parts;
+  int unit, parts;        // parts: that run at once
+  int most_parts;         // with late ones, where the page table is wide enough for so many tiles
   bool by_seq;            // parts are sequences
   // workspace
   int4* meta;             // [parts]: what the join of part p does, see there
@@ -57,15 +61,29 @@ struct PagedAttnArgs {
   float* first_o;         // [parts][units][warps][unit][D]: see below
   uint32_t* status;
 };
-// The line cut into `active` parts, the first ones a tile longer where it does not divide.
+// A line cut into `n` parts, the first ones a tile longer where it does not divide.
 struct Parts {
   unsigned size, more;  // tiles of a part; parts that have one more
-  __device__ Parts(unsigned total, unsigned active) : size(total / active), more(total - size * active) {}
+  __device__ Parts(unsigned total, unsigned n) : size(total / n), more(total - size * n) {}
   __device__ unsigned begin(unsigned p) const { return p * size + min(p, more); }
-  __device__ int of(unsigned tile) const {
+  __device__ unsigned of(unsigned tile) const {
     const unsigned longer = more * (size + 1);
     return tile < longer ? tile / (size + 1) : more + (tile - longer) / size;
   }
+};
+// The line of all tiles: its parts at first, which run at once, and behind them late parts, which the SMs take up as they finish.  SMs that share
+// a way to memory with more others are slower by a third: with equal parts alone the others wait for them.
+struct Line {
+  unsigned firsts, early, active;  // first parts, the tiles that they have together, parts in all
+  Parts first, late;
+  __device__ Line(unsigned total, unsigned parts, unsigned warps)
+      : firsts(min((total + PD_LEAST * warps - 1) / (PD_LEAST * warps), parts)),
+        early(total >= parts * warps * PD_MANY ? total - total / PD_LATE : total),
+        active(early < total ? 2 * parts : firsts),
+        first(early, firsts > 0 ? firsts : 1),
+        late(total - early, parts) {}
+  __device__ unsigned begin(unsigned p) const { return p < firsts ? first.begin(p) : early + late.begin(p - firsts); }
+  __device__ int of(unsigned tile) const { return tile < early ? first.of(tile) : firsts + late.of(tile - early); }
 };
 
 __device__ __forceinline__ uint32_t movmatrix(uint32_t x) {
@@ -176,7 +194,7 @@ paged_attention_kernel(const PagedAttnArgs a) {
       if (a.lse) a.lse[(long long)s * a.q_heads + h] = -INFINITY;
     }
   };
-  Parts parts(0, 1);
+  Line parts(0, 1, WARPS);
   unsigned c0 = 0, c1, w0;  // this part's tiles of the line; the first of this warp's
   auto warp_begin = [&](int w) { return c0 + (unsigned)((unsigned long long)(c1 - c0) * w / WARPS); };
   // the sequence that this warp's stretch begins in: its number, its length, its first tile
@@ -220,12 +238,11 @@ paged_attention_kernel(const PagedAttnArgs a) {
     if (part == 0 && (!alone || warp == 0))
       for (int s = s0; s < s1; ++s)
         if ((s == s0 ? n0 : length(s)) == 0) nothing(s);
-    const int active = (int)min((total + PD_LEAST * WARPS - 1) / (PD_LEAST * WARPS), (unsigned)a.parts);
-    if (part >= active) {
+    parts = Line(total, a.parts, WARPS);
+    if (part >= parts.active) {
       if (hu == 0 && threadIdx.x == 0) a.meta[part] = make_int4(0, 0, 0, 0);
       return;
     }
-    parts = Parts(total, active);
     c0 = parts.begin(part), c1 = parts.begin(part + 1);
     w0 = warp_begin(warp);
     if (alone) {
@@ -793,11 +810,11 @@ static PagedPlan paged_plan(const a3_handle* h) {
   const int units = h->m.n_kv_heads * p.groups;
   p.parts = h->sm_count / units;
   if (p.parts < 1) p.parts = 1;
-  const size_t slots = (size_t)p.parts * units * 2 * p.unit;
-  p.meta = align_up(sizeof(int4) * p.parts, 256);
+  const size_t slots = (size_t)2 * p.parts * units * 2 * p.unit;
+  p.meta = align_up(sizeof(int4) * 2 * p.parts, 256);
   p.ml = align_up(slots * sizeof(float2), 256);
   p.o = align_up(slots * h->m.head_dim * 4, 256);
-  p.bytes = p.meta + p.ml + p.o + (size_t)p.parts * units * PD_WARPS * p.unit * h->m.head_dim * 4;
+  p.bytes = p.meta + p.ml + p.o + (size_t)2 * p.parts * units * PD_WARPS * p.unit * h->m.head_dim * 4;
   return p;
 }
 
@@ -813,10 +830,10 @@ static int paged_launch(const a3_handle* h, const PagedAttnArgs& a, int units, c
   static SmemAttrOnce once;
   using C = PagedCfg<D, F8, NT>;
   A3_TRY(smem_attr_once(once, h->device, paged_attention_kernel<D, F8, NT, WHOLE>, C::SMEM));
-  A3_CUDA(launch_pdl(paged_attention_kernel<D, F8, NT, WHOLE>, dim3((a.by_seq ? a.n_seqs : a.parts) * units), dim3(C::THREADS), C::SMEM, st, a));
+  A3_CUDA(launch_pdl(paged_attention_kernel<D, F8, NT, WHOLE>, dim3((a.by_seq ? a.n_seqs : a.most_parts) * units), dim3(C::THREADS), C::SMEM, st, a));
   A3_LAUNCHED();
-  if (a.by_seq || a.parts == 1) return A3_OK;  // every sequence ends in the part that it begins in
-  A3_CUDA(launch_pdl(paged_join_kernel<D>, dim3(a.parts - 1, units, a.unit), dim3(32 * PJ_WARPS), a.parts * sizeof(float), st, a));
+  if (a.by_seq || a.most_parts == 1) return A3_OK;  // every sequence ends in the part that it begins in
+  A3_CUDA(launch_pdl(paged_join_kernel<D>, dim3(a.most_parts - 1, units, a.unit), dim3(32 * PJ_WARPS), a.most_parts * sizeof(float), st, a));
   return launched();
 }
 
@@ -857,6 +874,8 @@ extern "C" int a3_paged_attention(const a3_handle* h, const a3_paged_cache* cach
   a.out = (bf16*)p.out, a.lse = p.lse_out;
   a.q_heads = m.n_q_heads, a.kv_heads = m.n_kv_heads, a.group = m.n_q_heads / m.n_kv_heads;
   a.unit = plan.unit, a.groups = plan.groups, a.parts = plan.parts, a.by_seq = alone;
+  const int tile = PD_STAGE / 2 / (m.head_dim * (cache->type == A3_CACHE_E4M3 ? 1 : 2));
+  a.most_parts = (slots / tile + 1) * p.n_seqs >= (unsigned long long)plan.parts * PD_WARPS * PD_MANY ? 2 * plan.parts : plan.parts;
   if (!alone) {
     a.meta = (int4*)p.ws;
     a.part_ml = (float2*)((char*)p.ws + plan.meta);

@@ -214,6 +214,21 @@ def test_attention_lengths_and_pages(a3, size, lens, packed):
     check_attention(a3, eng, cache, table, lens, randn(g, len(lens), hq, d, std=2.0))
 
 
+@pytest.mark.parametrize("packed,lens", [(False, [50000, 1, 0, 40000, 25000, 33]), (True, [120000, 0, 100001, 5000])])
+def test_attention_with_late_parts(a3, packed, lens):
+    """So many tiles that a tenth of them is left to late parts; and the same table with so few that there are none of them."""
+    hq, hkv, d = SHAPES["g4"]
+    eng, g = engine(a3, "g4"), gen(22)
+    tile = 32 if packed else 16
+    warps = torch.cuda.get_device_properties(0).multi_processor_count // hkv * 8
+    assert sum(-(-n // tile) for n in lens) >= 48 * warps  # from there on there are late parts
+    table, n = make_table(g, lens, 32)
+    cache = a3.PagedCache(*make_pool(g, n, 32, hkv, d, packed))
+    q = randn(g, len(lens), hq, d, std=2.0)
+    check_attention(a3, eng, cache, table, lens, q)
+    check_attention(a3, eng, cache, table, [n // 1000 for n in lens], q)
+
+
 def test_attention_reads_nothing_behind_a_sequence(a3):
     """Entries behind the last slot hold NaN, table entries behind the last page name no page; pages apart, queries in a wider buffer."""
     for packed in (False, True):
