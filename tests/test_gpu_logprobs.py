@@ -108,6 +108,20 @@ def test_ruled_out_tokens(eng, dtype):
     check(eng, torch.full((2, 700), torch.finfo(dtype).min, dtype=dtype, device=DEV), None, 9)
 
 
+def test_ruled_out_beside_the_lowest_values(eng):
+    """A largest logit so low that the type has no number far below it: -inf still adds nothing at all."""
+    for dtype in (torch.float32, torch.bfloat16, torch.float16):
+        low = torch.finfo(dtype).min
+        for top in (low, low * (1 - torch.finfo(dtype).eps), low * 0.998, low * 0.99):
+            x = torch.full((2, 20000), -math.inf, dtype=dtype, device=DEV)
+            t = torch.tensor([4321, 0], dtype=torch.int32, device=DEV)
+            x[torch.arange(2), t.long()] = top
+            logprob, entropy, ids, lps = eng.token_logprobs(x, t, 2)
+            assert eng.device_status() == 0
+            assert logprob.tolist() == [0, 0] and entropy.tolist() == [0, 0] and lps.tolist() == [[0, -math.inf]] * 2
+            assert ids.tolist() == [[4321, 0], [0, 1]]
+
+
 def test_nearly_certain_tokens(eng):
     """One logit far above the others: what is missing from 1, and the entropy, come from the others alone.  Those that share the
     largest one's thread (1 in 512) are lost below 2^-24, hence 1 %."""
