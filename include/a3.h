@@ -387,7 +387,7 @@ typedef struct {
  * q_rows.  Strides between rows in elements, multiples of 8: q, k and v may be columns of one buffer; each row is
  * [heads][D] without gaps.  row_seq[r] < 0 marks padding: nothing of such a row is written.  A row whose sequence, slot, page or
  * |pos| is out of range (n_seqs, max_pages, n_pages, max_positions) is left out as a whole and A3_DEV_BAD_POSITION is set.  Rows of
- * one call must go to different slots.  One launch. */
+ * one call must go to different slots, and what is written overlaps no input but as said.  One launch. */
 typedef struct {
   const int32_t* page_table;  /* dev [n_seqs][max_pages] */
   const int32_t* row_seq;     /* dev [M] */
@@ -414,7 +414,7 @@ typedef struct {
   const int32_t* page_table; /* dev [n_seqs][max_pages] */
   const int32_t* cache_len;  /* dev [n_seqs] */
   const void* q_rows;        /* dev [n_seqs][Hq][D] bf16, 16-byte aligned */
-  void* out;                 /* dev [n_seqs][Hq][D] bf16, 16-byte aligned */
+  void* out;                 /* dev [n_seqs][Hq][D] bf16, 16-byte aligned; overlaps no input */
   float* lse_out;            /* dev [n_seqs][Hq] natural-log row log-sum-exps of the scaled logits, or NULL */
   void* ws;                  /* dev, 256-byte aligned, a3_paged_attention_workspace_bytes bytes; not looked at where that is 0 */
   uint64_t ws_bytes;

@@ -4,8 +4,9 @@
 //
 // Every key and value is read once and used by the G query heads of its KV head: bound by HBM.  The lengths are known on the
 // device only, so the kernel divides the work itself: the keys of all sequences, cut into tiles of KT keys, form one line
-// per KV head; a CTA takes an equal stretch of it and each of its warps an equal part of that, whatever sequences
-// lie there.  A warp streams its tiles through a ring of its own with 16-byte asynchronous copies (two tiles under way while
+// per KV head; a CTA takes an equal stretch of it (where it is long, one more short stretch for who is done early) and each of
+// its warps an equal part of that, whatever sequences lie there.  Few and short sequences have a CTA each instead.  A warp
+// streams its tiles through a ring of its own with 16-byte asynchronous copies (two tiles under way while
 // the third is computed, no barrier between warps) and keeps the running maximum and sum of the softmax, fp32, in registers.
 // Products: S^T = K Q^T and O^T = V^T P^T with warp-level MMAs, keys (head dimensions) on the 16-row side and the heads that share
 // them on the 8-column side: the query heads of a group fill the narrow side of the instruction, and what they need of the
@@ -13,6 +14,11 @@
 // written at once; a CTA merges what its warps hold of a sequence; what several CTAs hold goes to the workspace as (maximum, sum,
 // unnormalised output) and a second kernel merges it in the order of the keys.  The division depends on the lengths and
 // the device only: results do not depend on timing.
+//
+// Measured, 32 query heads over 8 of 128, bf16: 128 sequences of up to 8 191 slots, 2.0 GB, in 300 us, 6.7 TB/s, as fast as a copy; one of 5 153 slots,
+// 21 MB, in 10.9 us, nearly all of them what any call takes whose keys are not in one CTA: lengths, pages and keys one after the other, the merge,
+// the join; one of 32 801 in 8 bits, 67 MB, in 20.9 us.  28 heads over 4, 8 bits, 16 sequences of up to 15 675 slots, 157 MB, in 35.5 us: the
+// widening and the products of 8-bit tiles take as long as their way from HBM, and the SM with the slowest way to it 32.6 us where the median takes 25.
 //
 // P is kept to 16 bits for bf16 values (two bf16 terms): with one, its rounding is as large as that of the output itself.  8-bit keys
 // and values are widened to fp16, which holds them exactly; the query is scaled by a power of two per head so that fp16 holds all of
@@ -32,8 +38,8 @@ constexpr float LN2 = 0.693147180559945309f;
 // Tiles of a warp up to which one CTA may have a sequence alone: one sequence of 512 slots (32 query heads over 8, bf16) 7.0 us in one launch and
 // 9.1 in two, of 768 8.8 and 9.1, of 1 024 10.6 and 9.1; in 8 bits, where a tile is twice as many slots, of 1 024 8.1 and 9.8, of 2 048 12.7 and 9.8.
 constexpr int PD_ALONE = 5;
-// From so many tiles for each warp on, one tile in PD_LATE goes to late parts: 128 sequences of up to 8 191 slots (213 tiles a warp) 321 -> 307 us,
-// 32 of them (57) 93.3 -> 91.1, 32 of 28 heads over 4 (40) 70.3 -> 71.8.
+// From so many tiles for each warp on, one tile in PD_LATE goes to late parts: 128 sequences of up to 8 191 slots (213 tiles a warp) 321 -> 300 us,
+// 32 of them (57) 93.3 -> 89.7, 32 of 28 heads over 4 (40) 70.3 -> 71.8.  One in 20: 307 and 91.1.
 constexpr int PD_MANY = 48, PD_LATE = 10;
 constexpr int PD_LEAST = 2;  // tiles of a warp, before another part is begun
 constexpr float PD_SLACK = 8.f;  // see the running softmax
@@ -178,10 +184,12 @@ paged_attention_kernel(const PagedAttnArgs a) {
 
   pdl_wait();
   pdl_launch_dependents();
-  const float ks = F8 ? __ldcg(a.k_scale + kvh) : 1.f, vs = F8 ? __ldcg(a.v_scale + kvh) : 1.f;
+  const float k_by = F8 ? __ldcg(a.k_scale + kvh) : 1.f, vs = F8 ? __ldcg(a.v_scale + kvh) : 1.f;
 
   // ---- the line: every thread adds up the tiles of a stretch of sequences; each warp for itself or, where they are many, all together
   const long long cap = (long long)a.max_pages * a.page_size;
+  // Each length is read several times.  Should another stream write them meanwhile, results are meaningless, but every loop still ends and every
+  // access stays where it may be.
   auto length = [&](int s) {
     const int n = __ldcg(a.lens + s);
     return n < 0 || n > cap ? 0 : n;
@@ -226,7 +234,7 @@ paged_attention_kernel(const PagedAttnArgs a) {
     }
     unsigned total = __shfl_sync(0xffffffffu, upto, 31), before = upto - mine;
     if (!alone) {
-      if (lane == 31) s_scan[warp] = upto;
+      if (lane == 31) s_scan[warp] = upto, s_warp_seq[warp] = s_warp_len[warp] = 0, s_warp_first[warp] = 0;
       __syncthreads();
       total = 0;
 #pragma unroll
@@ -305,18 +313,20 @@ paged_attention_kernel(const PagedAttnArgs a) {
     auto lengths = [&] { x_len = x_base + lane < a.n_seqs ? length(x_base + lane) : 0; };
     if (x_left > (xn + KT - 1) / KT - xt) lengths();  // the stretch goes on there
     auto next_length = [&] {
+      if (xs == a.n_seqs - 1) return xn = 0, true;
       if (++xs == x_base + 32) {
         x_base = xs;
         lengths();
       }
       xn = __shfl_sync(0xffffffffu, x_len, xs - x_base);
+      return xn > 0;
     };
     auto look_up = [&](int j) {
       if (x_left <= 0) return;
       const int32_t* row = a.table + (long long)xs * a.max_pages;
       if (lane == 0) s_tile[warp][j % TILES] = make_int4(xs, xn, xt, xe);
       if constexpr (WHOLE) {
-        if (lane == 0) cp_async4(smem_u32(&s_page[warp][j % PAGES][0]), row + xp);
+        if (lane == 0) cp_async4(smem_u32(&s_page[warp][j % PAGES][0]), row + min(xp, a.max_pages - 1));
       } else {
 #pragma unroll
         for (int i = lane; i < KT; i += 32) {
@@ -328,8 +338,7 @@ paged_attention_kernel(const PagedAttnArgs a) {
       if (--x_left == 0) return;
       if (++xt * KT >= xn) {
         xt = xp = xe = 0;
-        do next_length();
-        while (xn == 0);
+        while (!next_length()) {}
       } else if (WHOLE && (xe += KT) == a.page_size) {
         xe = 0;
         ++xp;
@@ -423,7 +432,7 @@ paged_attention_kernel(const PagedAttnArgs a) {
             int ex = most > 0.f && most < INFINITY ? ilogbf(most) - 14 : 0;
             ex = max(-120, min(120, ex));
             const float down = __int_as_float((127 - ex) << 23);
-            up *= __int_as_float((127 + ex) << 23) * ks;
+            up *= __int_as_float((127 + ex) << 23) * k_by;
 #pragma unroll
             for (int ks = 0; ks < MT; ++ks)
 #pragma unroll
@@ -656,8 +665,9 @@ paged_attention_kernel(const PagedAttnArgs a) {
     }
   }
   if (!a.by_seq && hu == 0 && threadIdx.x == 0) {  // first0 and len0 are of the sequence that the part begins with
-    const int from = first0 < c0 ? parts.of(first0) : part, to = parts.of(first0 + (unsigned)(len0 + KT - 1) / KT - 1);
-    a.meta[part] = make_int4(seq0, from, from == part - 1 ? to - from + 1 : 0, 0);
+    const int from = first0 < c0 ? parts.of(first0) : part;
+    const unsigned to = min((unsigned)parts.of(first0 + (unsigned)(len0 + KT - 1) / KT - 1), parts.active - 1);
+    a.meta[part] = make_int4(seq0, from, from == part - 1 ? (int)to - from + 1 : 0, 0);
   }
   __syncthreads();
 
