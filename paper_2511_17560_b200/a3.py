@@ -9,7 +9,6 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-import struct
 from typing import Dict, List, Optional, Sequence
 
 import numpy as np
@@ -17,6 +16,8 @@ import torch
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "liba3.so")
 _lib = None
+_calls = None  # csrc/a3_calls.cpp, and the addresses of the library's functions that it calls
+_entry: Dict[str, int] = {}
 
 A3_OK = 0
 DEV_BAD_POSITION, DEV_NONFINITE_SCORE, DEV_WAIT_EXHAUSTED, DEV_UNSORTED_ROWS = 1, 2, 4, 8
@@ -94,12 +95,17 @@ class LayerPlan(C.Structure):
 
 
 def _load():
-    global _lib
+    global _lib, _calls
     if _lib is not None:
         return _lib
     if not os.path.exists(_LIB_PATH):
         raise ImportError(f"{_LIB_PATH} is missing: build it with `python -m paper_2511_17560_b200.build` "
                           "(there is no fallback path)")
+    try:
+        from . import a3_calls
+    except ImportError as e:
+        raise ImportError("a3_calls is missing or made for another torch: build it with `python -m paper_2511_17560_b200.build` "
+                          "(there is no fallback path)") from e
     lib = C.CDLL(_LIB_PATH)
     vp, i32, u64, sz = C.c_void_p, C.c_int, C.c_uint64, C.c_size_t
     lib.a3_create.argtypes = [C.POINTER(vp), C.POINTER(ModelDesc), C.POINTER(LayerWeights)]
@@ -154,7 +160,10 @@ def _load():
     lib.a3_kernel_class_name.argtypes = [i32]
     lib.a3_kernel_class_name.restype = C.c_char_p
     lib.a3_plan_layer.argtypes = [C.POINTER(ModelDesc), i32, i32, C.POINTER(LayerPlan)]
-    _lib = lib
+    a3_calls.set_error(A3Error)
+    for name in ("a3_paged_append", "a3_paged_attention_workspace_bytes", "a3_paged_attention", "a3_token_logprobs"):
+        _entry[name] = C.cast(getattr(lib, name), vp).value
+    _lib, _calls = lib, a3_calls
     return lib
 
 
@@ -286,14 +295,6 @@ class PagedCache:
         self.desc = PagedCacheDesc(k_pages.data_ptr(), v_pages.data_ptr(), stride * k_pages.element_size(), n, size, 1 if packed else 0, 0,
                                    _ptr(k_scale), _ptr(v_scale))
         self._ref = C.addressof(self.desc)
-
-
-# a3_paged_rows, a3_paged_queries and a3_logit_rows as one call's bytes: these calls are short on the device, and packing the
-# fields at once takes half the time of a ctypes argument each
-PAGED_ROWS = struct.Struct("@8P4Q4i")
-PAGED_QUERIES = struct.Struct("@6P2Q2ifi")
-LOGIT_ROWS = struct.Struct("@6PQ4i")
-_LOGIT_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
 class A3:
@@ -449,111 +450,31 @@ class A3:
                                       _ptr(ws), ws.numel(), _stream()), "a3_first_token")
         return logits, token
 
-    # ---- decoding on paged caches (these calls are short on the device: one condition for all that must hold, and no text before it fails)
+    # ---- decoding on paged caches (short on the device: csrc/a3_calls.cpp looks at the tensors, allocates and calls)
+    def _on(self, cache: PagedCache, where: str):
+        m = self.shape
+        if cache.n_kv_heads != m.n_kv_heads or cache.head_dim != m.head_dim or cache.device != self.device:
+            raise A3Error(-1, where + ": a cache of this model on the engine's device")
+        return cache._ref
+
     def paged_append(self, cache: PagedCache, page_table, row_seq, row_slot, k_rows, v_rows, q_rows=None, row_pos=None, rotate=True, q_out=None):
         """a3_paged_append; page_table [n_seqs][max_pages], rows [M][heads][D] (columns of a wider buffer will do); returns q_out or None."""
-        m, dev, i32, bf16 = self.shape, self.device, torch.int32, torch.bfloat16
-        rows, D = row_seq.shape, m.head_dim
-        if not (len(rows) == 1 and page_table.dim() == 2 and cache.n_kv_heads == m.n_kv_heads and cache.head_dim == D and cache.device == dev
-                and row_slot.shape == rows and page_table.dtype is row_seq.dtype is row_slot.dtype is i32
-                and page_table.device == dev and row_seq.device == dev and row_slot.device == dev
-                and page_table.is_contiguous() and row_seq.is_contiguous() and row_slot.is_contiguous()):
-            raise A3Error(-1, "a3_paged_append: cache of this model, and contiguous int32 page table and rows, on the engine's device")
-        if row_pos is not None and not (row_pos.shape == rows and row_pos.dtype is i32 and row_pos.device == dev and row_pos.is_contiguous()):
-            raise A3Error(-1, "a3_paged_append: row_pos")
-        M, = rows
-        kv_shape = (M, m.n_kv_heads, D)
-        if not (k_rows.shape == kv_shape and v_rows.shape == kv_shape and k_rows.dtype is v_rows.dtype is bf16 and k_rows.device == dev
-                and v_rows.device == dev):
-            raise A3Error(-1, "a3_paged_append: k_rows, v_rows: bf16 [M][Hkv][D] on the engine's device")
-        kr, kh, ke = k_rows.stride()
-        vr, vh, ve = v_rows.stride()
-        if M > 0 and not (ke == ve == 1 and (kh == vh == D or m.n_kv_heads == 1)):
-            raise A3Error(-1, "a3_paged_append: k_rows, v_rows: the heads of a row lie next to each other")
-        q = out = qr = outr = 0
-        if q_rows is not None:
-            q_shape = (M, m.n_q_heads, D)
-            if q_out is None:
-                q_out = q_rows.new_empty(q_shape)
-            if not (q_rows.shape == q_shape and q_out.shape == q_shape and q_rows.dtype is q_out.dtype is bf16 and q_rows.device == dev
-                    and q_out.device == dev):
-                raise A3Error(-1, "a3_paged_append: q_rows, q_out: bf16 [M][Hq][D] on the engine's device")
-            qr, qh, qe = q_rows.stride()
-            outr, oh, oe = q_out.stride()
-            if M > 0 and not (qe == oe == 1 and (qh == oh == D or m.n_q_heads == 1)):
-                raise A3Error(-1, "a3_paged_append: q_rows, q_out: the heads of a row lie next to each other")
-            q, out = q_rows.data_ptr(), q_out.data_ptr()
-        elif q_out is not None:
-            raise A3Error(-1, "a3_paged_append: q_out without q_rows")
-        if M == 1:  # one row has no distance to the next
-            kr = vr = m.n_kv_heads * D
-            qr = outr = m.n_q_heads * D
-        status = _load().a3_paged_append(self._h, cache._ref, PAGED_ROWS.pack(
-            page_table.data_ptr(), row_seq.data_ptr(), row_slot.data_ptr(), 0 if row_pos is None else row_pos.data_ptr(), q, k_rows.data_ptr(),
-            v_rows.data_ptr(), out, qr, kr, vr, outr, *page_table.shape, M, 1 if rotate else 0), _stream())
-        if status != A3_OK:
-            raise A3Error(status, "a3_paged_append")
-        return q_out
+        m = self.shape
+        return _calls.paged_append(_entry["a3_paged_append"], self._h.value, self._on(cache, "a3_paged_append"), _stream(), self.device,
+                                   m.n_q_heads, m.n_kv_heads, m.head_dim, page_table, row_seq, row_slot, k_rows, v_rows, q_rows, row_pos, rotate, q_out)
 
     def paged_attention(self, cache: PagedCache, page_table, cache_len, q_rows, scale=None, out=None, want_lse=False):
         """a3_paged_attention; returns (out [n_seqs][Hq][D], lse [n_seqs][Hq] or None).  The workspace is allocated by torch for
         this call alone, so that calls on several streams, or captured into several graphs, share none."""
-        m, dev, lib = self.shape, self.device, _load()
-        Hq, D = m.n_q_heads, m.head_dim
-        if not (page_table.dim() == 2 and cache_len.dim() == 1 and cache.n_kv_heads == m.n_kv_heads and cache.head_dim == D and cache.device == dev
-                and page_table.dtype is cache_len.dtype is torch.int32 and page_table.device == dev and cache_len.device == dev
-                and page_table.is_contiguous() and cache_len.is_contiguous()):
-            raise A3Error(-1, "a3_paged_attention: cache of this model, and contiguous int32 page table and lengths, on the engine's device")
-        n, max_pages = page_table.shape
-        shape = (n, Hq, D)
-        if not (cache_len.shape[0] == n and q_rows.shape == shape and q_rows.dtype is torch.bfloat16 and q_rows.device == dev):
-            raise A3Error(-1, "a3_paged_attention: q_rows: bf16 [n_seqs][Hq][D] on the engine's device")
-        qr, qh, qe = q_rows.stride()
-        if n > 0 and not (qe == 1 and (qh == D or Hq == 1)):
-            raise A3Error(-1, "a3_paged_attention: q_rows: the heads of a row lie next to each other")
-        if out is None:
-            out = torch.empty_like(q_rows, memory_format=torch.contiguous_format)
-        elif not (out.dtype is torch.bfloat16 and out.shape == shape and out.is_contiguous() and out.device == dev):
-            raise A3Error(-1, "a3_paged_attention: out")
-        lse = q_rows.new_empty((n, Hq), dtype=torch.float32) if want_lse else None
-        nbytes = lib.a3_paged_attention_workspace_bytes(self._h, cache._ref, n, max_pages)
-        ws = q_rows.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
-        status = lib.a3_paged_attention(self._h, cache._ref, PAGED_QUERIES.pack(
-            page_table.data_ptr(), cache_len.data_ptr(), q_rows.data_ptr(), out.data_ptr(), 0 if lse is None else lse.data_ptr(), 0 if ws is None else ws.data_ptr(), nbytes,
-            qr if n > 1 else Hq * D, n, max_pages, D ** -0.5 if scale is None else scale, 0), _stream())
-        if status != A3_OK:
-            raise A3Error(status, "a3_paged_attention")
-        return out, lse
+        m = self.shape
+        return _calls.paged_attention(_entry["a3_paged_attention"], _entry["a3_paged_attention_workspace_bytes"], self._h.value,
+                                      self._on(cache, "a3_paged_attention"), _stream(), self.device, m.n_q_heads, m.head_dim, page_table, cache_len, q_rows,
+                                      m.head_dim ** -0.5 if scale is None else scale, out, want_lse)
 
     def token_logprobs(self, logits, targets=None, n_top=0):
         """a3_token_logprobs on logits [M][vocab] (fp32, bf16 or fp16; rows may be apart); returns (logprob [M] or None without targets,
         entropy [M], top_ids [M][n_top] and top_logprobs [M][n_top], or None)."""
-        kind = _LOGIT_TYPES.get(logits.dtype)
-        if kind is None or logits.dim() != 2 or logits.device != self.device:
-            raise A3Error(-1, "a3_token_logprobs: logits [M][vocab] on the engine's device")
-        M, vocab = logits.shape
-        row, one = logits.stride()
-        if vocab == 0 or (one != 1 and vocab > 1):
-            raise A3Error(-1, "a3_token_logprobs: logits of a row lie next to each other")
-        logprob = ids = lps = None
-        given = logprob_at = ids_at = lps_at = 0
-        if targets is not None:
-            if not (targets.shape == (M,) and targets.dtype is torch.int32 and targets.device == self.device and targets.is_contiguous()):
-                raise A3Error(-1, "a3_token_logprobs: targets: contiguous int32 [M] on the engine's device")
-            logprob = logits.new_empty(M, dtype=torch.float32)
-            entropy = torch.empty_like(logprob)
-            given, logprob_at = targets.data_ptr(), logprob.data_ptr()
-        else:
-            entropy = logits.new_empty(M, dtype=torch.float32)
-        if n_top > 0:
-            lps = logits.new_empty((M, n_top), dtype=torch.float32)
-            ids = torch.empty_like(lps, dtype=torch.int32)
-            ids_at, lps_at = ids.data_ptr(), lps.data_ptr()
-        status = _load().a3_token_logprobs(self._h, LOGIT_ROWS.pack(logits.data_ptr(), given, logprob_at, entropy.data_ptr(), ids_at, lps_at,
-                                                                    row if M > 1 else vocab, kind, M, vocab, n_top), _stream())
-        if status != A3_OK:
-            raise A3Error(status, "a3_token_logprobs")
-        return logprob, entropy, ids, lps
+        return _calls.token_logprobs(_entry["a3_token_logprobs"], self._h.value, _stream(), self.device, logits, targets, n_top)
 
     def make_request(self, chunks, n_chunks, max_chunk_len, n_ctx, n_question, x0, k_fused, v_fused, ratio=0.15,
                      select_layer=1, n_system=0, forced_re=None, n_recompute=None, score_source=0, evict_capacity=0,

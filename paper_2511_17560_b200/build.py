@@ -1,4 +1,4 @@
-"""Builds liba3.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a.
+"""Builds, in-tree, liba3.so (the C-ABI CUDA library) with nvcc for sm_100a and a3_calls.so (the compiled part of the Python binding) with g++.
 
 Usage: python -m paper_2511_17560_b200.build [--force] [--verbose]
 """
@@ -7,12 +7,14 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "liba3.so")
+CALLS = os.path.join(PKG, "a3_calls.so")
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
          "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
@@ -27,6 +29,23 @@ def _stale(target, deps):
         return True
     t = os.path.getmtime(target)
     return any(os.path.getmtime(d) > t for d in deps)
+
+
+def build_calls(force: bool = False) -> str:
+    """a3_calls.so, against the headers and libraries of the torch that is installed."""
+    import torch
+
+    src, base = os.path.join(CSRC, "a3_calls.cpp"), os.path.dirname(torch.__file__)
+    if force or _stale(CALLS, [src, os.path.join(ROOT, "include", "a3.h"), os.path.join(base, "version.py")]):
+        inc = [os.path.join(base, "include"), os.path.join(base, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"]]
+        cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+               "-I", os.path.join(ROOT, "include")] + [a for i in inc for a in ("-isystem", i)]
+        cmd += [src, "-o", CALLS, "-L", os.path.join(base, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"]
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode:
+            sys.stderr.write(r.stdout + r.stderr)
+            raise RuntimeError("g++ failed for " + src)
+    return CALLS
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -48,8 +67,10 @@ def build(force: bool = False, verbose: bool = False) -> str:
                 raise RuntimeError("nvcc failed for " + src)
         return obj
 
-    with ThreadPoolExecutor(max_workers=8) as ex:
+    with ThreadPoolExecutor(max_workers=9) as ex:
+        calls = ex.submit(build_calls, force)
         objs = list(ex.map(compile_one, srcs))
+        calls.result()
     if force or _stale(LIB, objs):
         cmd = [NVCC, "-shared", "-o", LIB] + objs + ["-lcudart", "-lcuda"]
         r = subprocess.run(cmd, capture_output=True, text=True)

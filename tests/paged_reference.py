@@ -1,9 +1,14 @@
 """Plain forms in 64 bits of the calls on paged caches and of the log probabilities, with the error each may be off by."""
 import math
+import struct
 
 import torch
 
 E4M3_MAX = 448.0
+# a3_paged_rows, a3_paged_queries and a3_logit_rows as bytes, for calls of the library that the binding would not make
+PAGED_ROWS = struct.Struct("@8P4Q4i")
+PAGED_QUERIES = struct.Struct("@6P2Q2ifi")
+LOGIT_ROWS = struct.Struct("@6PQ4i")
 
 
 def turned(x, pos, theta, layout):

@@ -203,7 +203,7 @@ def test_refusals_of_the_library(a3, eng):
     f, i, t = torch.zeros((2, 64), device=DEV), torch.zeros((2, 64), dtype=torch.int32, device=DEV), torch.zeros(2, dtype=torch.int32, device=DEV)
     p = lambda v: v.data_ptr()  # noqa: E731
     good = dict(x=p(x), t=p(t), lp=p(f), e=p(f), ids=p(i), lps=p(f), stride=64, type=0, M=2, V=64, n=3)
-    call = lambda h=eng._h, **kw: lib.a3_token_logprobs(h, a3.LOGIT_ROWS.pack(*[0 if v is None else v for v in {**good, **kw}.values()]), 0)  # noqa: E731
+    call = lambda h=eng._h, **kw: lib.a3_token_logprobs(h, R.LOGIT_ROWS.pack(*[0 if v is None else v for v in {**good, **kw}.values()]), 0)  # noqa: E731
     assert lib.a3_token_logprobs(eng._h, None, 0) == -1
     a3.launch_count(reset=True)
     for kw in [dict(h=None), dict(x=None), dict(x=p(x) + 2), dict(stride=63), dict(M=-1), dict(V=0), dict(t=None), dict(lp=None), dict(n=-1),

@@ -434,7 +434,7 @@ def test_refusals_of_the_library(a3):
     p = lambda t: t.data_ptr()  # noqa: E731
     whole = lambda kw: [0 if v is None else v for v in kw.values()]  # noqa: E731
     good = dict(t=p(table), len=p(one), q=p(q), o=p(o), lse=None, ws=p(ws), b=nbytes, qs=hq * d, n=1, w=wide, scale=0.1, r=0)
-    attend = lambda h=eng._h, c=C.addressof(cache.desc), **kw: lib.a3_paged_attention(h, c, a3.PAGED_QUERIES.pack(*whole({**good, **kw})), 0)  # noqa: E731
+    attend = lambda h=eng._h, c=C.addressof(cache.desc), **kw: lib.a3_paged_attention(h, c, R.PAGED_QUERIES.pack(*whole({**good, **kw})), 0)  # noqa: E731
     assert attend() == 0 and attend(w=1, ws=None, b=0) == 0 and lib.a3_paged_attention(eng._h, cache._ref, None, 0) == -1 and lib.a3_paged_append(eng._h, cache._ref, None, 0) == -1
     a3.launch_count(reset=True)
     kept = []
@@ -454,7 +454,7 @@ def test_refusals_of_the_library(a3):
     assert attend(w=1 << 27) == -6 and attend(n=1 << 10, w=(1 << 20) + 1) == -6
     good_a = dict(t=p(table), seq=p(zero), slot=p(zero), pos=None, q=p(q), k=p(k), v=p(v), o=p(o), qs=hq * d, ks=hkv * d, vs=hkv * d, os=hq * d,
                   n=1, w=1, M=1, rot=1)
-    append = lambda h=eng._h, c=C.addressof(cache.desc), **kw: lib.a3_paged_append(h, c, a3.PAGED_ROWS.pack(*whole({**good_a, **kw})), 0)  # noqa: E731
+    append = lambda h=eng._h, c=C.addressof(cache.desc), **kw: lib.a3_paged_append(h, c, R.PAGED_ROWS.pack(*whole({**good_a, **kw})), 0)  # noqa: E731
     for kw in [dict(h=None), dict(c=None), dict(t=None), dict(n=-1), dict(w=-1), dict(seq=None), dict(slot=None), dict(k=None), dict(v=None),
                dict(q=None), dict(o=None), dict(M=-1), dict(k=p(k) + 2), dict(ks=hkv * d - 8), dict(vs=hkv * d + 1), dict(qs=8), dict(os=hq * d + 4), dict(ks=1 << 32)]:
         assert append(**kw) == -1, kw

@@ -1,8 +1,10 @@
 """What the binding of the paged-cache calls and of the log probabilities refuses, and what it hands on.  The library calls
 themselves are replaced; nothing here needs a GPU."""
 import ctypes
+import gc
 import os
 import subprocess
+import sys
 from dataclasses import replace
 
 import pytest
@@ -10,39 +12,34 @@ import torch
 
 from paper_2511_17560_b200 import a3
 from paper_2511_17560_b200 import workloads as W
-
-
-class Recorder:
-    def __init__(self, lib):
-        self._lib, self.calls = lib, []
-
-    def __getattr__(self, name):
-        return getattr(self._lib, name)
-
-    def a3_paged_attention_workspace_bytes(self, h, cache, n_seqs, max_pages):
-        return 512 if n_seqs > 1 else 0
-
-    def a3_paged_append(self, h, cache, rows, stream):
-        self.calls.append(a3.PAGED_ROWS.unpack(rows))
-        return 0
-
-    def a3_paged_attention(self, h, cache, queries, stream):
-        self.calls.append(a3.PAGED_QUERIES.unpack(queries))
-        return 0
-
-    def a3_token_logprobs(self, h, rows, stream):
-        self.calls.append(a3.LOGIT_ROWS.unpack(rows))
-        return 0
+from tests import paged_reference as R
 
 
 @pytest.fixture
 def eng(monkeypatch):
-    lib = Recorder(a3._load())
-    monkeypatch.setattr(a3, "_load", lambda: lib)
+    """An engine on the CPU whose library calls only note what they are given."""
+    a3._load()
+    calls, kept = [], []
+
+    def replace_call(name, packed):
+        def note(h, cache, fields, stream):
+            calls.append(packed.unpack(ctypes.string_at(fields, packed.size)))
+            return 0
+
+        put(name, note, ctypes.c_int, 4 if packed is not R.LOGIT_ROWS else 3)
+
+    def put(name, fn, result, n, *rest):
+        f = fn if n != 3 else lambda h, fields, stream: fn(h, None, fields, stream)
+        kept.append(ctypes.CFUNCTYPE(result, *[ctypes.c_void_p] * n, *rest)(f))
+        monkeypatch.setitem(a3._entry, name, ctypes.cast(kept[-1], ctypes.c_void_p).value)
+
+    for name, packed in [("a3_paged_append", R.PAGED_ROWS), ("a3_paged_attention", R.PAGED_QUERIES), ("a3_token_logprobs", R.LOGIT_ROWS)]:
+        replace_call(name, packed)
+    put("a3_paged_attention_workspace_bytes", lambda h, cache, n_seqs, max_pages: 512 if n_seqs > 1 else 0, ctypes.c_size_t, 2, ctypes.c_int, ctypes.c_int)
     monkeypatch.setattr(a3, "_stream", lambda: 0)
     e = a3.A3.__new__(a3.A3)
-    e.shape, e._h, e._ws, e.device = replace(W.TINY, n_q_heads=4, n_kv_heads=2), None, None, torch.device("cpu")
-    e.calls = lib.calls
+    e.shape, e._h, e._ws, e.device = replace(W.TINY, n_q_heads=4, n_kv_heads=2), ctypes.c_void_p(), None, torch.device("cpu")
+    e.calls, e.kept = calls, kept
     return e
 
 
@@ -132,12 +129,59 @@ def test_logprob_arguments(eng):
     assert len(eng.calls) == calls
 
 
+def test_arguments_of_other_kinds_and_statuses(eng, monkeypatch):
+    cache, table, lens = a3.PagedCache(pages(), pages()), torch.zeros((3, 2), dtype=torch.int32), i32(5, 0, 32)
+    q, x = torch.zeros((3, 4, 64), dtype=torch.bfloat16), torch.zeros((3, 80))
+    for bad in (None, 3, "x", [1, 2, 3], x.numpy()):
+        refused(eng.paged_append, cache, table, bad, lens, q[:, :2], q[:, 2:])
+        refused(eng.paged_append, cache, table, lens, lens, bad, q[:, 2:])
+        refused(eng.paged_attention, cache, bad, lens, q)
+        refused(eng.paged_attention, cache, table, lens, bad)
+        refused(eng.token_logprobs, bad)
+        if bad is not None:
+            refused(eng.paged_append, cache, table, lens, lens, q[:, :2], q[:, 2:], row_pos=bad)
+            refused(eng.paged_append, cache, table, lens, lens, q[:, :2], q[:, 2:], q_rows=bad)
+            refused(eng.paged_attention, cache, table, lens, q, out=bad)
+            refused(eng.token_logprobs, x, bad)
+    refused(eng.token_logprobs, x, None, 1 << 31)
+    for n in ("x", 1 << 70):
+        with pytest.raises((TypeError, OverflowError)):
+            eng.token_logprobs(x, None, n)
+    with pytest.raises(TypeError):
+        eng.paged_attention(cache, table, lens, q, scale="x")
+    refused(eng.paged_append, cache, table.to_sparse(), lens, lens, q[:, :2], q[:, 2:])
+    assert eng.calls == []
+    fails = ctypes.CFUNCTYPE(ctypes.c_int, *[ctypes.c_void_p] * 4)(lambda *a: -3)
+    monkeypatch.setitem(a3._entry, "a3_paged_attention", ctypes.cast(fails, ctypes.c_void_p).value)
+    with pytest.raises(a3.A3Error) as e:
+        eng.paged_attention(cache, table, lens, q)
+    assert e.value.status == -3 and "a3_paged_attention" in str(e.value)
+
+
+def test_results_are_the_callers_alone(eng):
+    """No tensor outlives its last use, and none is freed before: counted on tensors that the calls allocate and on those that they are given."""
+    cache, table, lens = a3.PagedCache(pages(), pages()), torch.zeros((3, 2), dtype=torch.int32), i32(5, 0, 32)
+    q, x = torch.zeros((3, 4, 64), dtype=torch.bfloat16), torch.zeros((3, 80))
+    given = torch.empty_like(q)
+    before = [sys.getrefcount(o) for o in (table, lens, q, x, given)]
+    for _ in range(50):
+        out, lse = eng.paged_attention(cache, table, lens, q, want_lse=True)
+        assert sys.getrefcount(out) == sys.getrefcount(lse) == 2
+        assert eng.paged_attention(cache, table, lens, q, out=given)[0] is given
+        assert eng.paged_append(cache, table, lens, lens, q[:, :2], q[:, 2:], q_rows=q, q_out=given) is given
+        assert all(sys.getrefcount(o) == 2 + 1 for o in eng.token_logprobs(x, lens, 4))  # the list's iterator holds it too
+        refused(eng.paged_attention, cache, table, lens, x)
+    del out, lse
+    gc.collect()  # frames of the refusals
+    assert before == [sys.getrefcount(o) for o in (table, lens, q, x, given)]
+
+
 def test_structs_match_the_header(tmp_path):
     """The packed forms have the header's size and order: each field's place as the C compiler sees it."""
     fields = {"a3_paged_rows": ("page_table row_seq row_slot row_pos q_rows k_rows v_rows q_out q_stride k_stride v_stride q_out_stride n_seqs max_pages M "
-                                "rotate", a3.PAGED_ROWS),
-              "a3_paged_queries": ("page_table cache_len q_rows out lse_out ws ws_bytes q_stride n_seqs max_pages scale reserved", a3.PAGED_QUERIES),
-              "a3_logit_rows": ("logits targets logprob_out entropy_out top_ids_out top_logprobs_out row_stride type M vocab n_top", a3.LOGIT_ROWS)}
+                                "rotate", R.PAGED_ROWS),
+              "a3_paged_queries": ("page_table cache_len q_rows out lse_out ws ws_bytes q_stride n_seqs max_pages scale reserved", R.PAGED_QUERIES),
+              "a3_logit_rows": ("logits targets logprob_out entropy_out top_ids_out top_logprobs_out row_stride type M vocab n_top", R.LOGIT_ROWS)}
     lines = ['printf("%zu\\n", sizeof(a3_paged_cache));'] + [f'printf("%zu\\n", offsetof(a3_paged_cache, {f}));' for f, _ in a3.PagedCacheDesc._fields_]
     want = [ctypes.sizeof(a3.PagedCacheDesc)] + [getattr(a3.PagedCacheDesc, f).offset for f, _ in a3.PagedCacheDesc._fields_]
     for name, (names, packed) in fields.items():
