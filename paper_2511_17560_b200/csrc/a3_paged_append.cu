@@ -5,8 +5,8 @@
 // the cosines and sines: its loads do not depend on where the row goes, so they are on their way while the page is looked up.
 //
 // Bound by HBM where rows are many, by latency where they are few.  Measured on heads of 128: 17 871 rows of 28 heads over 4, bf16, 342 MB, in
-// 57.5 us, 5.9 TB/s; 32 768 rows of 8 KV heads into 8 bits, 202 MB, in 40.8 us, 4.9 TB/s (the conversion's instructions are half of the
-// time); 256 rows of a batch 2.6 us, one row 1.8 us.
+// 57.5 us, 5.9 TB/s; 32 768 rows of 8 KV heads into 8 bits, 202 MB, in 39.5 us, 5.1 TB/s (rotation and conversion issue for half of
+// the time); 256 rows of a batch 2.6 us, one row 1.8 us.
 #include <cuda_fp8.h>
 
 #include "a3_internal.cuh"
@@ -15,8 +15,10 @@
 namespace a3 {
 
 constexpr int PA_THREADS = 128;
-constexpr int PA_MIN = 5;     // CTAs per SM: 96 registers hold the four heads and their cosines
-constexpr int PA_HEADS = 4;   // of a thread where rows are many
+// CTAs per SM: 96 registers hold the four heads and their cosines.  The rows in 8 bits above 39.5 us with 5, 44 with 4 or 6; those in bf16 57.5, 58.7
+// and 61.7.  Two heads for each thread and 7 CTAs 44.5 and 60.7.
+constexpr int PA_MIN = 5;
+constexpr int PA_HEADS = 4;  // of a thread where rows are many
 // Units per SM up to which a thread moves one head, three CTAs: 128 rows of 32 heads over 8, bf16 (332 units per SM), 2.42 us with one
 // head and 2.52 with four, 160 rows (415) 2.95 and 2.61, 2 048 rows 16.3 and 10.7.
 constexpr int PA_ONE = 3 * PA_THREADS;
@@ -80,6 +82,7 @@ paged_append_kernel(const AppendArgs a) {
     const bf16 *q = a.q + r * a.q_stride + 8 * j, *k = a.k + r * a.k_stride + 8 * j - a.q_heads * D;
     const bf16* v = a.v + r * a.v_stride + 8 * j - (a.q_heads + a.kv_heads) * D;
     uint4 x[HEADS][2];
+    float scale[HEADS];
 #pragma unroll
     for (int i = 0; i < HEADS; ++i) {
       const int h = h0 + i * stride;
@@ -87,6 +90,7 @@ paged_append_kernel(const AppendArgs a) {
         const bf16* src = (h < a.q_heads ? q : h < a.q_heads + a.kv_heads ? k : v) + h * D;
         x[i][0] = __ldcs(reinterpret_cast<const uint4*>(src));
         x[i][1] = __ldcs(reinterpret_cast<const uint4*>(src + D / 2));
+        if (F8 && h >= a.q_heads) scale[i] = __ldg(h < a.q_heads + a.kv_heads ? a.k_scale + (h - a.q_heads) : a.v_scale + (h - a.q_heads - a.kv_heads));
       }
     }
     const bool turned = a.rotate && pos < 0, live = page != -2;
@@ -139,7 +143,7 @@ paged_append_kernel(const AppendArgs a) {
         const int kh = h - a.q_heads - (is_v ? a.kv_heads : 0);
         char* dst = (is_v ? a.v_pages : a.k_pages) + place + kh * (D * (F8 ? 1 : 2));
         if (F8) {
-          const float by = __frcp_rn(__ldg((is_v ? a.v_scale : a.k_scale) + kh));
+          const float by = __frcp_rn(scale[i]);
           *reinterpret_cast<uint2*>(dst) = pack8_e4m3(f, by);
           *reinterpret_cast<uint2*>(dst + D / 2) = pack8_e4m3(f + 8, by);
         } else {
