@@ -2,7 +2,8 @@
 // looking at some ten tensors from Python took longer than that.  Each function checks its tensors, allocates the results with torch, fills
 // the header's struct and makes the one call.  It is given the address of the library's function, so that it links against torch alone.
 //
-// Measured on the host for the whole call, launch included, here and with the same checks in Python through ctypes: see the binding.
+// Measured on the host, launch included, with the same checks in Python and here: one appended row 7.7 and 3.6 us, one short sequence 11.1 and
+// 5.8, one of 5 153 slots (two launches) 15.3 and 8.6, one row of logits with five alternatives (four results) 13.3 and 7.7.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <limits.h>

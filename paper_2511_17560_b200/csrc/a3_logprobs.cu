@@ -13,9 +13,9 @@
 // through again, in the ring where that still holds the row, else from L2, a warp together on one thread's elements.  What reaches the
 // bound, usually 1-2 n elements, is ranked by counting.
 //
-// Measured, bf16: 2 048 rows of 128 256, 525 MB, one alternative each, 87 us while the clock holds (6.0 TB/s) and 102 us repeated without a pause,
+// Measured, bf16: 2 048 rows of 128 256, 525 MB, one alternative each, 87 us while the clock holds (6.0 TB/s) and 96-103 us repeated without a pause,
 // when the power limit lowers it to 1.6 GHz: an exponential and some seven other instructions for each element fill the SM as the way from HBM does.  65 rows
-// of 152 064 with 20 alternatives each 13.0 us, one row of 128 256 in fp32 7.6 us: latency, the ranking after the pass among it.
+// of 152 064 with 20 alternatives each 12.6 us, one row of 128 256 in fp32 7.4 us: latency, the ranking after the pass among it.
 #include <cuda_fp16.h>
 
 #include "a3_internal.cuh"
