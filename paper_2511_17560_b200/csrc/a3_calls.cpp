@@ -64,9 +64,10 @@ template <typename F, typename... A>
 void call(PyObject* fn, const char* where, A... args) {
   const F f = (F)address(fn);
   need(f != nullptr, where);
-  int status;
-  Py_BEGIN_ALLOW_THREADS status = f(args...);
-  Py_END_ALLOW_THREADS if (status != A3_OK) throw Refused{status, where};
+  PyThreadState* state = PyEval_SaveThread();
+  const int status = f(args...);
+  PyEval_RestoreThread(state);
+  if (status != A3_OK) throw Refused{status, where};
 }
 
 template <typename Body>
