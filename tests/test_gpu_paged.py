@@ -1,5 +1,6 @@
 """Appending rows to a paged cache and attention of one new token over it, against plain forms in 64 bits."""
 import math
+import threading
 from dataclasses import replace
 
 import pytest
@@ -378,6 +379,40 @@ def test_calls_on_another_stream(a3):
                 got.append(eng.paged_attention(cache, table, lens, q)[0])
     torch.cuda.synchronize()
     assert all(torch.equal(want, o) for o in got)
+
+
+def test_calls_from_two_threads(a3):
+    """Each thread decodes on a stream and a pool of its own through one engine; the calls let the other thread run while they launch."""
+    hq, hkv, d = SHAPES["g4"]
+    eng, g = engine(a3, "g4"), gen(23)
+    sets = []
+    for i in range(2):
+        lens = [700 + 900 * i, 3, 2500]
+        table, n = make_table(g, lens, 16)
+        kp, vp, _, _ = make_pool(g, n, 16, hkv, d, False)
+        sets.append((a3.PagedCache(kp, vp), table, ints(range(3)), ints([x - 1 for x in lens]), ints(lens), randn(g, 3, hq, d), randn(g, 3, hkv, d),
+                     randn(g, 3, hkv, d), randn(g, 3, 20000), ints([0, 19999, 5])))
+
+    def step(cache, table, seq, slot, lens, q, k, v, x, t):
+        return (*eng.paged_attention(cache, table, lens, eng.paged_append(cache, table, seq, slot, k, v, q_rows=q), want_lse=True), *eng.token_logprobs(x, t, 4))
+
+    want = [step(*s) for s in sets]
+    torch.cuda.synchronize()
+    got = [[], []]
+
+    def work(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            got[i] = [step(*sets[i]) for _ in range(200)][-20:]
+            torch.cuda.current_stream().synchronize()
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for th in threads:
+        th.start()
+    for th in threads:
+        th.join()
+    for i in range(2):
+        assert len(got[i]) == 20 and all(torch.equal(bits(a), bits(b)) for step_out in got[i] for a, b in zip(want[i], step_out))
+    assert eng.device_status() == 0
 
 
 def test_attention_without_pages(a3):
