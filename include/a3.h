@@ -423,7 +423,7 @@ typedef struct {
   float scale;
   int32_t reserved;
 } a3_paged_queries;
-/* For this cache, so many sequences and this width of the page table; 0 where few and short sequences need none. */
+/* For this cache, so many sequences and this width of the page table; 0 where sequences are so few and short that none is needed. */
 size_t a3_paged_attention_workspace_bytes(const a3_handle* h, const a3_paged_cache* cache, int n_seqs, int max_pages);
 int a3_paged_attention(const a3_handle* h, const a3_paged_cache* cache, const a3_paged_queries* queries, a3_stream stream);
 

@@ -5,7 +5,7 @@
 // Every key and value is read once and used by the G query heads of its KV head: bound by HBM.  The lengths are known on the
 // device only, so the kernel divides the work itself: the keys of all sequences, cut into tiles of KT keys, form one line
 // per KV head; a CTA takes an equal stretch of it (where it is long, one more short stretch for who is done early) and each of
-// its warps an equal part of that, whatever sequences lie there.  Few and short sequences have a CTA each instead.  A warp
+// its warps an equal part of that, whatever sequences lie there.  Few and short sequences have CTAs of their own instead.  A warp
 // streams its tiles through a ring of its own with 16-byte asynchronous copies (two tiles under way while
 // the third is computed, no barrier between warps) and keeps the running maximum and sum of the softmax, fp32, in registers.
 // Products: S^T = K Q^T and O^T = V^T P^T with warp-level MMAs, keys (head dimensions) on the 16-row side and the heads that share
@@ -16,8 +16,8 @@
 // the device only: results do not depend on timing.
 //
 // Measured, 32 query heads over 8 of 128, bf16: 128 sequences of up to 8 191 slots, 2.0 GB, in 300 us, 6.7 TB/s, as fast as a copy; one of 5 153 slots,
-// 21 MB, in 10.9 us, nearly all of them what any call takes whose keys are not in one CTA: lengths, pages and keys one after the other, the merge,
-// the join; one of 32 801 in 8 bits, 67 MB, in 20.9 us.  28 heads over 4, 8 bits, 16 sequences of up to 15 675 slots, 157 MB, in 35.5 us: the
+// 21 MB, in 10.2 us by eight CTAs for each KV head, nearly all of them lengths, pages and keys one after the other and the two merges; where a
+// second launch joins, that is 2 us more; one of 32 801 in 8 bits, 67 MB, in 20.9 us.  28 heads over 4, 8 bits, 16 sequences of up to 15 675 slots, 157 MB, in 35.5 us: the
 // widening and the products of 8-bit tiles take as long as their way from HBM, and the SM with the slowest way to it 32.6 us where the median takes 25.
 //
 // P is kept to 16 bits for bf16 values (two bf16 terms): with one, its rounding is as large as that of the output itself.  8-bit keys
@@ -35,9 +35,14 @@ namespace a3 {
 constexpr int PD_WARPS = 8;      // of a CTA, one per SM
 constexpr int PD_STAGE = 8192;   // bytes of a tile: keys in the lower half, values in the upper
 constexpr float LN2 = 0.693147180559945309f;
-// Tiles of a warp up to which one CTA may have a sequence alone: one sequence of 512 slots (32 query heads over 8, bf16) 7.0 us in one launch and
-// 9.1 in two, of 768 8.8 and 9.1, of 1 024 10.6 and 9.1; in 8 bits, where a tile is twice as many slots, of 1 024 8.1 and 9.8, of 2 048 12.7 and 9.8.
-constexpr int PD_ALONE = 5;
+// A sequence (of a unit of heads) has CTAs to itself, without a second launch, where that leaves a warp PD_ALONE tiles at most; as many, up to PD_CTAS
+// in a cluster, as run at once, but no more once a warp has PD_FEW.  On the device, 32 query heads over 8, with CTAs of its own and on
+// the line: one sequence of 600 slots 6.3 us and 9.1, 2 500 7.6 and 9.7, 5 100 9.5 and 10.3; 8 of 1 200 10.5 and 12.7; 4 of 2 500 11.5 and 13.6;
+// 16 of 760, a CTA and 6 tiles a warp each, 11.5 and 16.2; in 8 bits, whose tiles are twice the slots and the work, one of 1 200 6.9 and 10.5, of 5 100 10.8 and 11.6, and with 4 tiles of 9 000 12.8 and 12.1.
+// Fewer CTAs, up to PD_ALONE tiles a warp: 600 slots 7.4, 2 500 8.9; 1 200 in 8 bits 9.4.
+constexpr int PD_CTAS = 8;
+constexpr int PD_ALONE = 6, PD_ALONE_E4M3 = 3;
+constexpr int PD_FEW = 2, PD_FEW_E4M3 = 1;
 // From so many tiles for each warp on, one tile in PD_LATE goes to late parts: 128 sequences of up to 8 191 slots (213 tiles a warp) 321 -> 300 us,
 // 32 of them (57) 93.3 -> 89.7, 32 of 28 heads over 4 (40) 70.3 -> 71.8.  One in 20: 307 and 91.1.
 constexpr int PD_MANY = 48, PD_LATE = 10;
@@ -59,7 +64,7 @@ struct PagedAttnArgs {
   int q_heads, kv_heads, group, groups;  // groups: CTAs' head units per KV head, of `unit` query heads at most
   int unit, parts;        // parts: that run at once
   int most_parts;         // with late ones, where the page table is wide enough for so many tiles
-  bool by_seq;            // parts are sequences
+  int by_seq;             // CTAs that have one sequence (of a unit) to themselves, a cluster where more than one; 0: parts of the line
   // workspace
   int4* meta;             // [parts]: what the join of part p does, see there
   float* part_o;          // [parts][units][2][unit][D]
@@ -123,6 +128,16 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// Where a variable of this CTA's shared memory lies in CTA `rank` of the cluster.
+template <typename V>
+__device__ __forceinline__ const V* of_rank(const V* p, unsigned rank) {
+  const V* q;
+  asm("mapa.u64 %0, %1, %2;" : "=l"(q) : "l"(p), "r"(rank));
+  return q;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 __device__ __forceinline__ uint32_t pack2h(float a, float b) {
   __half2 t = __floats2half2_rn(a, b);
   return *reinterpret_cast<uint32_t*>(&t);
@@ -163,10 +178,11 @@ paged_attention_kernel(const PagedAttnArgs a) {
   __shared__ int s_page[WARPS][PAGES][KEYS], s_ent[WARPS][PAGES][KEYS];  // page of a tile or, where it may cross pages, page and entry of each key
   __shared__ SlotInfo s_info[2 * WARPS];
   __shared__ float s_m[2 * WARPS][HN], s_l[2 * WARPS][HN];
+  __shared__ float2 s_whole[HN];  // (m, l) of the CTA's share of a cluster's sequence; l -1: it has none
   static_assert(!WHOLE || NT > 1 || C::SMEM + sizeof(s_scan) + sizeof(s_warp_first) + sizeof(s_warp_seq) + sizeof(s_warp_len) + sizeof(s_tile) + sizeof(s_page) +
-                                        sizeof(s_ent) + sizeof(s_info) + sizeof(s_m) + sizeof(s_l) <= 195 * 1024, "see above");
+                                        sizeof(s_ent) + sizeof(s_info) + sizeof(s_m) + sizeof(s_l) + sizeof(s_whole) <= 195 * 1024, "see above");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int units = a.kv_heads * a.groups, hu = blockIdx.x % units, part = blockIdx.x / units;
+  const int units = a.kv_heads * a.groups, ctas = max(a.by_seq, 1), rank = blockIdx.x % ctas, hu = blockIdx.x / ctas % units, part = blockIdx.x / ctas / units;
   const int kvh = hu / a.groups, h0 = kvh * a.group + hu % a.groups * a.unit, hn = min(a.unit, (kvh + 1) * a.group - h0);
   char* ring = smem + warp * C::RING;
   const uint32_t ring_u = smem_u32(ring);
@@ -207,12 +223,14 @@ paged_attention_kernel(const PagedAttnArgs a) {
   // the sequence that this warp's stretch begins in: its number, its length, its first tile
   int seq0 = 0, len0 = 0;
   unsigned first0 = 0;
-  if (a.by_seq) {  // a CTA for each sequence and head unit: a line of its own
-    seq0 = part, len0 = length(part), c1 = (len0 + KT - 1) / KT;
+  if (a.by_seq) {  // a sequence and head unit has CTAs of its own, each an equal stretch
+    seq0 = part, len0 = length(part);
     if (len0 == 0) {
-      if (threadIdx.x == 0) nothing(part);
-      return;
+      if (threadIdx.x == 0 && rank == 0) nothing(part);
+      if (ctas == 1) return;  // in a cluster nobody leaves alone
     }
+    const unsigned total = (len0 + KT - 1) / KT;
+    c0 = total * (unsigned)rank / ctas, c1 = total * (unsigned)(rank + 1) / ctas;
     w0 = warp_begin(warp);
   } else {
     const bool alone = a.n_seqs <= 32;
@@ -604,7 +622,7 @@ paged_attention_kernel(const PagedAttnArgs a) {
           for (int e = 0; e < 2; ++e)
 #pragma unroll
             for (int x = 4; x < 32; x <<= 1) l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], x);
-        if (piece0 == 0 && ct == tiles - 1) {
+        if (piece0 == 0 && ct == tiles - 1 && ctas == 1) {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -674,6 +692,8 @@ paged_attention_kernel(const PagedAttnArgs a) {
   __syncthreads();
 
   // ---- what the warps hold of one sequence, merged
+  if (ctas > 1 && threadIdx.x < HN) s_whole[threadIdx.x] = make_float2(-INFINITY, -1.f);
+  if (ctas > 1) __syncthreads();
   int seqs[2 * WARPS];
 #pragma unroll
   for (int i = 0; i < 2 * WARPS; ++i) seqs[i] = s_info[i].seq;
@@ -717,7 +737,10 @@ paged_attention_kernel(const PagedAttnArgs a) {
         const int i = __ffs(b) - 1;
         add(ex2(s_m[i][h] - ref), s_l[i][h], *reinterpret_cast<const float4*>(first_o + i / 2 * a.unit * D + C::out_at(h, d)));
       }
-      if (!began && !goes_on) {
+      if (ctas > 1) {  // in the place of warp 0's, which nobody else reads
+        *reinterpret_cast<float4*>(smem + C::out_at(h, d) * 4) = o;
+        if (d == 0) s_whole[h] = make_float2(mm, ll);
+      } else if (!began && !goes_on) {
         const float g = ll == 0.f ? 0.f : 1.f / ll;
         const long long at = (long long)info.seq * a.q_heads + h0 + h;
         *reinterpret_cast<uint2*>(a.out + at * D + d) = make_uint2(pack2(o.x * g, o.y * g), pack2(o.z * g, o.w * g));
@@ -728,6 +751,42 @@ paged_attention_kernel(const PagedAttnArgs a) {
       }
     }
   }
+
+  // ---- what the CTAs of a cluster hold of it, merged by the first
+  if (ctas == 1) return;
+  cluster_sync();
+  if (rank == 0) {
+    for (int x = threadIdx.x; x < hn * (D / 4); x += C::THREADS) {
+      const int h = x / (D / 4), d = x % (D / 4) * 4;
+      float2 ml[PD_CTAS];
+      float4 v[PD_CTAS];
+#pragma unroll
+      for (int i = 0; i < PD_CTAS; ++i) {
+        ml[i] = make_float2(-INFINITY, -1.f);
+        if (i < ctas) {
+          ml[i] = *of_rank(&s_whole[h], i);
+          v[i] = *of_rank(reinterpret_cast<const float4*>(smem + C::out_at(h, d) * 4), i);
+        }
+      }
+      float mm = -INFINITY, ll = 0.f;
+#pragma unroll
+      for (int i = 0; i < PD_CTAS; ++i) mm = fmaxf(mm, ml[i].x);
+      const float ref = mm == -INFINITY ? 0.f : mm;
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < PD_CTAS; ++i) {
+        if (ml[i].y == -1.f) continue;
+        const float g = ex2(ml[i].x - ref);
+        ll += g * ml[i].y;
+        o.x += g * v[i].x, o.y += g * v[i].y, o.z += g * v[i].z, o.w += g * v[i].w;
+      }
+      const float g = ll == 0.f ? 0.f : 1.f / ll;
+      const long long at = (long long)part * a.q_heads + h0 + h;
+      *reinterpret_cast<uint2*>(a.out + at * D + d) = make_uint2(pack2(o.x * g, o.y * g), pack2(o.z * g, o.w * g));
+      if (a.lse && d == 0) a.lse[at] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * LN2;
+    }
+  }
+  cluster_sync();  // the others' memory is there until it has been read
 }
 
 // Block (p, unit, head): the sequence that part p begins with, if it began in the part before, from all parts that hold some of it:
@@ -830,11 +889,16 @@ static PagedPlan paged_plan(const a3_handle* h) {
   return p;
 }
 
-// A CTA for each sequence and head unit needs no second launch; worth it where all of them run at once and none has many tiles, whatever the
-// lengths turn out to be within the page table's width.
-static bool paged_alone(const a3_handle* h, const PagedPlan& plan, const a3_paged_cache* cache, int n_seqs, int max_pages) {
-  const int row = h->m.head_dim * (cache->type == A3_CACHE_E4M3 ? 1 : 2), tile = PD_STAGE / 2 / row;  // slots of a tile
-  return (long long)n_seqs * h->m.n_kv_heads * plan.groups <= h->sm_count && (long long)max_pages * cache->page_size <= (long long)PD_ALONE * PD_WARPS * tile;
+// CTAs for each sequence and head unit, 0 where the line has them; whatever the lengths turn out to be within the page table's width.
+static int paged_alone(const a3_handle* h, const PagedPlan& plan, const a3_paged_cache* cache, int n_seqs, int max_pages) {
+  const bool f8 = cache->type == A3_CACHE_E4M3;
+  const long long slots = (long long)max_pages * cache->page_size, seqs = (long long)n_seqs * h->m.n_kv_heads * plan.groups;
+  const long long round = (long long)PD_WARPS * (PD_STAGE / 2 / (h->m.head_dim * (f8 ? 1 : 2)));  // slots of a CTA whose warps have a tile each
+  // clusters leave SMs unused: 12 of eight CTAs run at once, 16 do not (8 sequences of 5 100 17.2 us and on the line 12.6)
+  auto fit = [&](int ctas) { return seqs * ctas <= h->sm_count - (ctas == 1 ? 0 : ctas < 8 ? h->sm_count / 8 : h->sm_count / 4); };
+  int ctas = 1;
+  while (ctas < PD_CTAS && slots > (f8 ? PD_FEW_E4M3 : PD_FEW) * round * ctas && fit(2 * ctas)) ctas *= 2;
+  return slots <= (f8 ? PD_ALONE_E4M3 : PD_ALONE) * round * ctas && fit(ctas) ? ctas : 0;
 }
 
 template <int D, bool F8, int NT, bool WHOLE>
@@ -842,7 +906,8 @@ static int paged_launch(const a3_handle* h, const PagedAttnArgs& a, int units, c
   static SmemAttrOnce once;
   using C = PagedCfg<D, F8, NT>;
   A3_TRY(smem_attr_once(once, h->device, paged_attention_kernel<D, F8, NT, WHOLE>, C::SMEM));
-  A3_CUDA(launch_pdl(paged_attention_kernel<D, F8, NT, WHOLE>, dim3((a.by_seq ? a.n_seqs : a.most_parts) * units), dim3(C::THREADS), C::SMEM, st, a));
+  A3_CUDA(launch_pdl_cluster(a.by_seq > 1 ? a.by_seq : 1, paged_attention_kernel<D, F8, NT, WHOLE>, dim3((a.by_seq ? a.n_seqs * a.by_seq : a.most_parts) * units),
+                             dim3(C::THREADS), C::SMEM, st, a));
   A3_LAUNCHED();
   if (a.by_seq || a.most_parts == 1) return A3_OK;  // every sequence ends in the part that it begins in
   A3_CUDA(launch_pdl(paged_join_kernel<D>, dim3(a.most_parts - 1, units, a.unit), dim3(32 * PJ_WARPS), a.most_parts * sizeof(float), st, a));
@@ -856,7 +921,7 @@ using namespace a3;
 extern "C" size_t a3_paged_attention_workspace_bytes(const a3_handle* h, const a3_paged_cache* cache, int n_seqs, int max_pages) {
   if (!h || !cache || n_seqs <= 0 || max_pages < 0) return 0;
   const PagedPlan plan = paged_plan(h);
-  return paged_alone(h, plan, cache, n_seqs, max_pages) ? 0 : plan.bytes;
+  return paged_alone(h, plan, cache, n_seqs, max_pages) > 0 ? 0 : plan.bytes;
 }
 
 extern "C" int a3_paged_attention(const a3_handle* h, const a3_paged_cache* cache, const a3_paged_queries* queries, a3_stream stream) {
@@ -873,7 +938,7 @@ extern "C" int a3_paged_attention(const a3_handle* h, const a3_paged_cache* cach
   const a3_model_desc& m = h->m;
   if (p.q_stride < (uint64_t)m.n_q_heads * m.head_dim || p.q_stride % 8 || p.q_stride > (uint64_t)1 << 31) return A3_EINVAL;
   const PagedPlan plan = paged_plan(h);
-  const bool alone = paged_alone(h, plan, cache, p.n_seqs, p.max_pages);
+  const int alone = paged_alone(h, plan, cache, p.n_seqs, p.max_pages);
   if (!alone && (!p.ws || (uintptr_t)p.ws & 255)) return A3_EINVAL;
   if (!alone && p.ws_bytes < plan.bytes) return A3_EWORKSPACE;
   PagedAttnArgs a{};

@@ -429,6 +429,24 @@ def test_attention_without_pages(a3):
 
 
 @pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("shape", ["g4", "g2", "g10_64"])
+def test_attention_where_a_cluster_has_a_sequence(a3, shape, packed):
+    """Page tables as wide as one, two, four and eight CTAs take, and wider; in each, lengths that leave CTAs of a cluster, or all, without keys."""
+    hq, hkv, d = SHAPES[shape]
+    eng, g = engine(a3, shape), gen(24)
+    for n in (1, 3):
+        for width in (40, 100, 300, 1300, 2600, 5100, 6200):
+            table, pages = make_table(g, [width] * n, 16)
+            cache = a3.PagedCache(*make_pool(g, pages, 16, hkv, d, packed))
+            for lens in ([width] * n, [1, 0, width // 2][:n], [0, 17, width - 1][:n], [33, 32, 31][:n]):
+                q = randn(g, n, hq, d, std=2.0)
+                check_attention(a3, eng, cache, table, lens, q)
+                first = eng.paged_attention(cache, table, ints(lens), q, want_lse=True)
+                for a, b in zip(first, eng.paged_attention(cache, table, ints(lens), q, want_lse=True)):
+                    assert torch.equal(bits(a), bits(b))
+
+
+@pytest.mark.parametrize("packed", [False, True])
 def test_attention_where_one_cta_or_many_have_a_sequence(a3, packed):
     """The same sequences behind page tables of different widths: alone in a CTA each, and on the line of all CTAs."""
     hq, hkv, d = SHAPES["g4"]
