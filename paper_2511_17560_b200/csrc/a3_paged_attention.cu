@@ -38,8 +38,9 @@ constexpr float LN2 = 0.693147180559945309f;
 // A sequence (of a unit of heads) has CTAs to itself, without a second launch, where that leaves a warp PD_ALONE tiles at most; as many, up to PD_CTAS
 // in a cluster, as run at once, but no more once a warp has PD_FEW.  On the device, 32 query heads over 8, with CTAs of its own and on
 // the line: one sequence of 600 slots 6.3 us and 9.1, 2 500 7.6 and 9.7, 5 100 9.5 and 10.3; 8 of 1 200 10.5 and 12.7; 4 of 2 500 11.5 and 13.6;
-// 16 of 760, a CTA and 6 tiles a warp each, 11.5 and 16.2; in 8 bits, whose tiles are twice the slots and the work, one of 1 200 6.9 and 10.5, of 5 100 10.8 and 11.6, and with 4 tiles of 9 000 12.8 and 12.1.
-// Fewer CTAs, up to PD_ALONE tiles a warp: 600 slots 7.4, 2 500 8.9; 1 200 in 8 bits 9.4.
+// 16 of 760, a CTA and 6 tiles a warp each, 11.5 and 16.2; in 8 bits, whose tiles are twice the slots and the work, one of 1 200 6.9 and 10.5,
+// of 5 100 10.8 and 11.6, and of 9 000 with more than PD_ALONE_E4M3 tiles a warp 12.8 and 12.1.  With no more CTAs than PD_ALONE asks for: 600
+// slots 7.4, 2 500 8.9, 1 200 in 8 bits 9.4.
 constexpr int PD_CTAS = 8;
 constexpr int PD_ALONE = 6, PD_ALONE_E4M3 = 3;
 constexpr int PD_FEW = 2, PD_FEW_E4M3 = 1;
