@@ -5,8 +5,9 @@
 //
 // The logits are read once: bound by HBM where rows are many, by latency where they are few.  A row belongs to one CTA or, where rows
 // are fewer than the device holds, to a cluster whose CTAs join their parts through distributed shared memory.  Each thread keeps the
-// running (M, s, w) of its own elements.  s is carried without the 1 of one largest element and ends in log1p: where one token
-// has nearly all of the probability, what it lacks of 1 and the entropy come from the other tokens alone.
+// running (M, s, w) of its own elements.  From the warps' sums on, s is carried without the 1 of one largest element, and ends in log1p: where one
+// token has nearly all of the probability, what it lacks of 1 and the entropy come from the other tokens alone.  The thread that holds it has
+// added its other elements to that 1; in such a row, and in no other, they are added up once more without it.
 //
 // The alternatives come from the same pass: the n-th largest of the threads' maxima (of the 32 that are left when each warp gives its largest) is
 // a bound that at least n elements reach, and only the threads whose own maximum reaches it - little more than n of them - are gone
@@ -32,6 +33,9 @@ struct LpCfg {
 };
 static_assert(LP_TOP <= 32, "the bound is the n-th largest of them");
 constexpr float LOG2E = 1.44269504088896341f;
+// Where the other elements of the warp that has the largest one come to an eighth of it or more, an addition to a sum that holds its 1 is off by
+// 9 x 2^-24 of theirs at most; below, the largest one's thread adds its elements up once more.
+constexpr float LP_CERTAIN = 0.125f;
 constexpr float LP_FAR = -200.f;  // exp of it is 0 in fp32, and unlike that of -inf or of the lowest value its product with that 0 is 0 too
 
 struct LogprobArgs {
@@ -381,9 +385,31 @@ logprobs_kernel(const LogprobArgs a) {
     if (s_red[0][i] > most) most = s_red[0][i], holder = i;
   {
     const uint32_t these = __ballot_sync(0xffffffffu, m == most);
+    const int who = __ffs(these) - 1;
     const float d = fmaxf(m - most, LP_FAR), g = m > -INFINITY ? lp_ex2(d * LOG2E) : 0.f;
-    const float ps = warp_sum(g * (warp == holder && lane == __ffs(these) - 1 ? s - 1.f : s));
+    float ps = warp_sum(g * (warp == holder && lane == who ? s - 1.f : s));
     const float pw = warp_sum(m > -INFINITY ? g * (w + s * d) : 0.f);
+    // What the holder's other elements add beside its 1 is lost below 2^-24: where that is much of what all others add, the warp goes through
+    // them again and leaves the 1 out.
+    if (warp == holder && most > -INFINITY && ps < LP_CERTAIN) {
+      const bool kept = v1 - v0 <= LP_STAGES * LP_U * THREADS;  // all of the CTA's vectors are still in the ring
+      float others = lane == who ? 0.f : g * s;
+      int ones = 0;  // elements that are as large
+      auto count = [&](float f) {
+        if (f == most)
+          ++ones;
+        else
+          others += lp_ex2(fmaxf(f - most, LP_FAR) * LOG2E);
+      };
+      for (int v = warp * 32 + who + lane * THREADS; v < v1 - v0; v += 32 * THREADS) {
+        float f[VE];
+        Logit<T>::unpack(kept ? ring[v] : __ldcg(xv + v0 + v), f);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) count(f[e]);
+      }
+      if (lane == who && single >= 0) count(Logit<T>::one(x + single));
+      ps = warp_sum(others) + (float)((int)__reduce_add_sync(0xffffffffu, ones) - 1);
+    }
     if (lane == 0) s_red[1][warp] = ps, s_red[2][warp] = pw;
   }
 

@@ -213,3 +213,52 @@ def test_refusals_of_the_library(a3, eng):
     assert a3.launch_count() == 0
     assert call() == 0 and call(e=None) == 0 and call(n=0, ids=None, lps=None) == 0 and call(t=None, lp=None) == 0
     assert eng.device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("M,V", [(1, 128256), (40, 40000), (400, 4096), (400, 40000), (310, 128256)])
+def test_two_tokens_are_left(eng, dtype, M, V):
+    """Two finite logits `gap` apart, as a grammar leaves them: neighbours, and as far apart as the elements of one thread lie, with the
+    first elements in front of the first 16-byte boundary or not.  With s = exp(-gap): log p = -log1p(s), entropy log1p(s) + gap s / (1 + s).
+    The exponential's argument is rounded twice (2^-24 of gap each), the exponential and log1p are off by 2^-22 each, the sums here by 2^-22."""
+    size = torch.finfo(dtype).bits // 8
+    for first in (0, 1):
+        wide = torch.full((M, V + 16), -math.inf, dtype=dtype, device=DEV)
+        x = wide[:, first:first + V]
+        for apart in [1, 3] + [t * 16 // size for t in (64, 128, 256)]:
+            for at, gap in ((0, 18.0), (8, 16.75), (1027, 24.5), (V - 1 - apart, 40.0), (V // 2, 9.0)):
+                if at + apart >= V:
+                    continue
+                for top in (at, at + apart):  # the larger one first, and last
+                    wide.fill_(-math.inf)
+                    x[:, at] = x[:, at + apart] = 2.0 - gap
+                    x[:, top] = 2.0
+                    t = torch.full((M,), top, dtype=torch.int32, device=DEV)
+                    logprob, entropy, ids, lps = eng.token_logprobs(x, t, 2)
+                    s = math.exp(-gap)
+                    want, h = -math.log1p(s), math.log1p(s) + gap * s / (1 + s)
+                    rel = gap * 2.0 ** -23 + 2.0 ** -20
+                    assert ((logprob.double() - want).abs() <= rel * -want).all(), (first, apart, at, gap, logprob[0].item(), want)
+                    assert ((entropy.double() - h).abs() <= rel * h).all(), (first, apart, at, gap, entropy[0].item(), h)
+                    assert torch.equal(logprob, lps[:, 0]) and (ids == torch.tensor([top, 2 * at + apart - top], device=DEV)).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("M,V", [(1, 512), (400, 512), (400, 20000), (300, 128256), (2, 128256)])
+def test_one_token_above_a_full_row(eng, dtype, M, V):
+    """One logit `up` above the largest of the others, from hardly likelier to certain.  What the others sum up to is a sum of V / 64 terms at
+    most in a thread, each added with 2^-24 of the sum so far.  Where the largest one's 1 is among them, what they add is an eighth of it at
+    least: 9 x 2^-24 for each, relative to the others alone."""
+    x, t = rows(M, V, dtype, M + V, std=1.0)
+    at = t.long()[:, None]
+    for up in (0.0, 1.0, 3.0, 6.0, 9.0, 14.0, 20.0, 30.0, 50.0):
+        y = x.clone()
+        y.scatter_(1, at, (x.float().amax(1, keepdim=True) + up).to(dtype))
+        logprob, entropy, _, _ = eng.token_logprobs(y, t, 1)
+        d = y.double() - y.double().gather(1, at)
+        e = d.exp().scatter(1, at, 0.0)
+        s = e.sum(1)
+        h = torch.log1p(s) - (e * d).sum(1) / (1 + s)
+        rel = (up + 12) * 2.0 ** -23 + 2.0 ** -20 + 9 * (V / 64 + 64) * 2.0 ** -24
+        assert ((logprob.double() + torch.log1p(s)).abs() <= rel * s).all(), (up, ((logprob.double() + torch.log1p(s)) / s).abs().max().item())
+        assert ((entropy.double() - h).abs() <= rel * (h + s)).all(), (up, ((entropy.double() - h) / h).abs().max().item())
