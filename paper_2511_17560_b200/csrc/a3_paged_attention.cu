@@ -22,7 +22,8 @@
 //
 // P is kept to 16 bits for bf16 values (two bf16 terms): with one, its rounding is as large as that of the output itself.  8-bit keys
 // and values are widened to fp16, which holds them exactly; the query is scaled by a power of two per head so that fp16 holds all of
-// its bits down to 2^-29 of its largest element, and P as fp16 is off by 2^-12 at most.
+// its bits down to 2^-29 of its largest element.  P as one fp16 term is off by 2^-11 of itself, an eighth of the output's rounding, or by 2^-32 of
+// the reference's weight where it is far below it; a second term would be half as many products again.
 #include <cuda_fp16.h>
 
 #include <type_traits>
@@ -49,6 +50,9 @@ constexpr int PD_FEW = 2, PD_FEW_E4M3 = 1;
 constexpr int PD_MANY = 48, PD_LATE = 10;
 constexpr int PD_LEAST = 2;  // tiles of a warp, before another part is begun
 constexpr float PD_SLACK = 8.f;  // see the running softmax
+// Weights beside 8-bit values are 2^PD_LIFT times as large as their logits say, up to 2^15: fp16 keeps 11 bits of a weight down to 2^-21 of the reference's, and
+// half a step of what is below is 2^-32 of it.
+constexpr float PD_LIFT = 7.f;
 
 struct PagedAttnArgs {
   const char *k_pages, *v_pages;
@@ -171,6 +175,7 @@ __global__ void __launch_bounds__(PagedCfg<D, F8, NT>::THREADS, 1)
 paged_attention_kernel(const PagedAttnArgs a) {
   using C = PagedCfg<D, F8, NT>;
   constexpr int KT = C::KT, CH = C::CH, HN = C::HN, SUB = KT / 16, MT = D / 16, WARPS = C::WARPS;
+  constexpr float LIFT = F8 ? PD_LIFT : 0.f;
   extern __shared__ __align__(1024) char smem[];
   __shared__ unsigned s_scan[WARPS], s_warp_first[WARPS];
   __shared__ int s_warp_seq[WARPS], s_warp_len[WARPS];
@@ -525,8 +530,8 @@ paged_attention_kernel(const PagedAttnArgs a) {
       };
       load_v(0);
 
-      // ---- running softmax: the reference m need not be the maximum, it only has to be near it.  It is raised, over the lanes that
-      // share a head and with everything rescaled, when a logit is more than 2^8 above it; weights are 256 at most.
+      // ---- running softmax: the reference need not be the maximum, it only has to be near it.  It is raised, over the lanes that
+      // share a head and with everything rescaled, when a logit's weight is more than 2^8 of its.  m is the logit of weight 1, LIFT below it.
       const int left = cn - ct * KT;  // keys from here on
       bool grew = false;
 #pragma unroll
@@ -537,7 +542,7 @@ paged_attention_kernel(const PagedAttnArgs a) {
           for (int e = 0; e < 4; ++e) {
             const float t = s[sub][nt][e] * cq[nt][e & 1];
             s[sub][nt][e] = t;
-            grew |= t > m[nt][e & 1] + PD_SLACK;
+            grew |= t > m[nt][e & 1] + (PD_SLACK + LIFT);
           }
       if (left < KT) {  // the sequence ends in this tile; what `grew` made of the rows behind it only raises the reference needlessly
 #pragma unroll
@@ -553,11 +558,12 @@ paged_attention_kernel(const PagedAttnArgs a) {
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            float now = m[nt][e];
+            float now = -INFINITY;
 #pragma unroll
             for (int sub = 0; sub < SUB; ++sub) now = fmaxf(now, fmaxf(s[sub][nt][e], s[sub][nt][e + 2]));
 #pragma unroll
             for (int x = 4; x < 32; x <<= 1) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, x));
+            now = fmaxf(m[nt][e], now - LIFT);
             const float f = now == -INFINITY ? 1.f : ex2(m[nt][e] - now);
             m[nt][e] = now;
             l[nt][e] *= f;

@@ -467,6 +467,38 @@ def test_attention_where_one_cta_or_many_have_a_sequence(a3, packed):
     assert a3.launch_count() == 3
 
 
+# ------------------------------------------------------------------ values far apart, and infinite ones
+
+
+@pytest.mark.parametrize("lens", [[1000], [3000] * 200, [20000, 5]])
+def test_attention_in_8_bits_of_many_small_weights(a3, lens):
+    """The first key far above all others, whose weights are e^-gap of its own and whose values are 1 where its own is 0: the output is what the small
+    weights add up to, w n' / (1 + w n').  A weight is off by 2^-11 of itself or, where fp16 has fewer bits for it, by half a step of 2^-24 beside a largest
+    weight of 2^7 at least: 2^-32.  The logits' own errors are R.attention's."""
+    hq, hkv, d = SHAPES["g2"]
+    eng, g = engine(a3, "g2"), gen(30)
+    table, n = make_table(g, lens, 32)
+    f8 = torch.float8_e4m3fn
+    for gap in (17.5, 12.0, 14.5, 20.0):
+        kp, vp = torch.zeros((n, 32, hkv, d), device=DEV), torch.ones((n, 32, hkv, d), device=DEV)
+        for s in range(len(lens)):
+            kp[table[s, 0].long(), 0, :, 0] = 4.0
+            vp[table[s, 0].long(), 0] = 0.0
+        one = torch.ones(hkv, device=DEV)
+        cache = a3.PagedCache(kp.to(f8), vp.to(f8), one, one)
+        q = torch.zeros((len(lens), hq, d), dtype=torch.bfloat16, device=DEV)
+        q[..., 0] = 1.0
+        out, lse = eng.paged_attention(cache, table, ints(lens), q, scale=gap / 4, want_lse=True)
+        assert eng.device_status() == 0
+        for s, m in enumerate(lens):
+            small = (m - 1) * math.exp(-gap)
+            want = small / (1 + small)
+            delta = gap * d * 2.0 ** -23 + (m + 8) * 2.0 ** -24
+            tol = want * (2.0 ** -8 + 2.0 ** -11 + 2 * delta) + m * 2.0 ** -32
+            assert ((out[s].double() - want).abs() <= tol).all(), (gap, s, m, out[s, 0, 0].item(), want)
+            assert ((lse[s].double() - gap - math.log1p(small)).abs() <= delta + 32 * 2.0 ** -22).all()
+
+
 # ------------------------------------------------------------------ refusals
 
 
