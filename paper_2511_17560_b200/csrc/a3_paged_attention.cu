@@ -143,6 +143,12 @@ __device__ __forceinline__ const V* of_rank(const V* p, unsigned rank) {
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// Two bf16, neither above its number (of numbers from 0 on).
+__device__ __forceinline__ uint32_t pack2_down(float a, float b) {
+  uint32_t y;
+  asm("cvt.rz.bf16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(b), "f"(a));
+  return y;
+}
 __device__ __forceinline__ uint32_t pack2h(float a, float b) {
   __half2 t = __floats2half2_rn(a, b);
   return *reinterpret_cast<uint32_t*>(&t);
@@ -586,10 +592,11 @@ paged_attention_kernel(const PagedAttnArgs a) {
             if constexpr (F8) {
               hi[sub][nt][e] = movmatrix(pack2h(p0, p1));
             } else {
-              const uint32_t h = pack2(p0, p1);
+              // the upper term is rounded down and the lower one is 2^-20 of the weight at least: an infinite value times either is that infinity
+              const uint32_t h = pack2_down(p0, p1);
               const float2 back = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&h));
               hi[sub][nt][e] = movmatrix(h);
-              lo[sub][nt][e] = movmatrix(pack2(p0 - back.x, p1 - back.y));
+              lo[sub][nt][e] = movmatrix(pack2(fmaxf(p0 - back.x, p0 * 0x1p-20f), fmaxf(p1 - back.y, p1 * 0x1p-20f)));
             }
           }
       }

@@ -499,6 +499,35 @@ def test_attention_in_8_bits_of_many_small_weights(a3, lens):
             assert ((lse[s].double() - gap - math.log1p(small)).abs() <= delta + 32 * 2.0 ** -22).all()
 
 
+@pytest.mark.parametrize("lens", [[40], [700, 3], [2500, 2], [9000, 0, 17]])
+def test_attention_of_infinite_values(a3, lens):
+    """A value of +inf makes that dimension +inf wherever its weight is above 0, -inf likewise, both together NaN; the other dimensions are as before."""
+    hq, hkv, d = SHAPES["g4"]
+    eng, g = engine(a3, "g4"), gen(31)
+    table, n = make_table(g, lens, 16)
+    kp, vp, _, _ = make_pool(g, n, 16, hkv, d, False)
+    cache, q = a3.PagedCache(kp, vp), randn(g, len(lens), hq, d)
+    clean, clean_lse = eng.paged_attention(cache, table, ints(lens), q, want_lse=True)
+    for where in (0, 33, lens[0] - 1):
+        at = (table[0, where // 16].long(), where % 16)
+        old = vp[at].clone()
+        vp[at[0], at[1], :, 5], vp[at[0], at[1], :, 100], vp[at[0], at[1], :, 64] = math.inf, -math.inf, math.inf
+        other = (table[0, (lens[0] - 2) // 16].long(), (lens[0] - 2) % 16)
+        old2 = vp[other].clone()
+        vp[other[0], other[1], :, 64] = -math.inf
+        out, lse = eng.paged_attention(cache, table, ints(lens), q, want_lse=True)
+        assert eng.device_status() == 0
+        assert (out[0, :, 5] == math.inf).all() and (out[0, :, 100] == -math.inf).all() and out[0, :, 64].isnan().all()
+        out[0, :, [5, 64, 100]] = clean[0, :, [5, 64, 100]]
+        assert torch.equal(bits(out), bits(clean)) and torch.equal(bits(lse), bits(clean_lse))
+        vp[other], vp[at] = old2, old
+    # a weight of 0 beside a value near the largest number adds nothing
+    q[0, :, 0] = 4.0
+    kp[table[0, 0].long(), 1], kp[table[0, 0].long(), 1, :, 0] = 0.0, -400.0
+    vp[table[0, 0].long(), 1] = 3e38
+    check_attention(a3, eng, cache, table, lens, q)
+
+
 # ------------------------------------------------------------------ refusals
 
 
