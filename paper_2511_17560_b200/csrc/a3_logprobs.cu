@@ -9,7 +9,7 @@
 // token has nearly all of the probability, what it lacks of 1 and the entropy come from the other tokens alone.  The thread that holds it has
 // added its other elements to that 1; in such a row, and in no other, they are added up once more without it.
 //
-// The alternatives come from the same pass: the n-th largest of the threads' maxima (of the 32 that are left when each warp gives its largest) is
+// The alternatives come from the same pass: the n-th largest of the threads' maxima (of the 32 that are left when each warp gives its largest), exactly, is
 // a bound that at least n elements reach, and only the threads whose own maximum reaches it - little more than n of them - are gone
 // through again, in the ring where that still holds the row, else from L2, a warp together on one thread's elements.  What reaches the
 // bound, usually 1-2 n elements, is ranked by counting.
@@ -87,6 +87,7 @@ struct Logit<float> {
   static constexpr int VE = 4;
   static constexpr float LOWEST = -3.40282347e38f, ORDINARY = LOWEST;
   static constexpr uint32_t NONE = 0xff800000u;
+  static constexpr int LAST_BIT = 0;
   __device__ static uint4 max_of(uint4 a, uint4 b) { return make_uint4(two(a.x, b.x), two(a.y, b.y), two(a.z, b.z), two(a.w, b.w)); }
   __device__ static uint32_t two(uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }
   __device__ static float largest(uint4 v) { return __uint_as_float(two(two(v.x, v.y), two(v.z, v.w))); }
@@ -106,6 +107,7 @@ struct Logit<bf16> {
   static constexpr int VE = 8;
   static constexpr float LOWEST = -3.38953139e38f, ORDINARY = LOWEST;
   static constexpr uint32_t NONE = 0xff80ff80u;  // a word of -inf
+  static constexpr int LAST_BIT = 16;            // of a value's bits in fp32
   __device__ static uint4 max_of(uint4 a, uint4 b) { return make_uint4(two(a.x, b.x), two(a.y, b.y), two(a.z, b.z), two(a.w, b.w)); }
   __device__ static uint32_t two(uint32_t a, uint32_t b) {
     uint32_t y;
@@ -129,6 +131,7 @@ struct Logit<__half> {
   static constexpr int VE = 8;
   static constexpr float LOWEST = -65504.f, ORDINARY = LOWEST - LP_FAR;
   static constexpr uint32_t NONE = 0xfc00fc00u;
+  static constexpr int LAST_BIT = 13;
   __device__ static uint4 max_of(uint4 a, uint4 b) { return make_uint4(two(a.x, b.x), two(a.y, b.y), two(a.z, b.z), two(a.w, b.w)); }
   __device__ static uint32_t two(uint32_t a, uint32_t b) {
     uint32_t y;
@@ -221,7 +224,7 @@ logprobs_kernel(const LogprobArgs a) {
   constexpr int VE = Logit<T>::VE;
   extern __shared__ __align__(16) uint4 ring[];
   __shared__ float s_red[3][WARPS];
-  __shared__ uint32_t s_kept[32];
+  __shared__ __align__(16) uint32_t s_kept[32];
   __shared__ unsigned long long s_cand[LP_CAP], s_best[WARPS];
   __shared__ int s_count, s_n_found;
   __shared__ uint8_t s_found[THREADS];
@@ -425,20 +428,23 @@ logprobs_kernel(const LogprobArgs a) {
     }
   };
   if (n > 0) {
-    // A bound that n threads' maxima reach: the n-th largest of those kept, or of all where not every thread has a vector (the upper 16 bits:
-    // a lower bound does as well).  Of one element alone, it is it.
+    // The n-th largest of the threads' maxima that were kept, or of all where not every thread has a vector: n elements reach it.  To the last bit of the
+    // type: of logits far from zero, whose spread is a small part of them, nearly all would reach a bound of fewer.  Of one element alone, it is it.
     if (n == 1) {
       bound = ordered(most);
     } else if (v1 - v0 >= THREADS) {
+      // an element's place is how many are better: a lane for each of the 32
       const uint32_t kept = s_kept[lane];
-#pragma unroll 1
-      for (int bit = 31; bit >= 16; --bit) {
-        const uint32_t c = bound | 1u << bit;
-        if (__popc(__ballot_sync(0xffffffffu, kept >= c)) >= n) bound = c;
+      int better = 0;
+#pragma unroll
+      for (int i = 0; i < 32; i += 4) {
+        const uint4 other = *reinterpret_cast<const uint4*>(s_kept + i);
+        better += (other.x > kept) + (other.y > kept) + (other.z > kept) + (other.w > kept);
       }
+      bound = __reduce_min_sync(0xffffffffu, better < n ? kept : 0xffffffffu);
     } else {
 #pragma unroll 1
-      for (int bit = 31; bit >= 16; --bit) {
+      for (int bit = 31; bit >= Logit<T>::LAST_BIT; --bit) {
         const uint32_t c = bound | 1u << bit;
         if (__syncthreads_count(mine >= c) >= n) bound = c;
       }

@@ -262,3 +262,31 @@ def test_one_token_above_a_full_row(eng, dtype, M, V):
         rel = (up + 12) * 2.0 ** -23 + 2.0 ** -20 + 9 * (V / 64 + 64) * 2.0 ** -24
         assert ((logprob.double() + torch.log1p(s)).abs() <= rel * s).all(), (up, ((logprob.double() + torch.log1p(s)) / s).abs().max().item())
         assert ((entropy.double() - h).abs() <= rel * (h + s)).all(), (up, ((entropy.double() - h) / h).abs().max().item())
+
+
+def test_a_shift_of_all_logits_costs_no_time(eng):
+    """The alternatives of rows far from zero are found as fast as those of rows around it (once, 1 000 in the logits took several times as long).
+    The values of both rows are multiples of 2^-10, so the shift loses nothing."""
+    def elapsed(x, n):
+        best = []
+        for _ in range(7):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            for _ in range(20):
+                eng.token_logprobs(x, None, n)
+            b.record()
+            torch.cuda.synchronize()
+            best.append(a.elapsed_time(b))
+        return sorted(best)[3]
+
+    for dtype, shift, M, V in ((torch.float32, 1000.0, 1, 128256), (torch.float32, 6000.0, 300, 30000), (torch.float16, 1000.0, 300, 30000), (torch.float32, 6000.0, 64, 3000)):
+        x, _ = rows(M, V, torch.float32, 12, std=2.5)
+        x = ((x * 1024).round() / 1024).to(dtype)
+        y = (x.float() + shift).to(dtype)
+        x = (y.float() - shift).to(dtype)
+        check(eng, y, None, 20)
+        check(eng, y[:1, 1:4097], None, 20)  # threads without a vector where V allows it
+        assert torch.equal(eng.token_logprobs(x, None, 20)[2], eng.token_logprobs(y, None, 20)[2])
+        base, shifted = elapsed(x, 20), elapsed(y, 20)
+        print(f"{dtype} {M} x {V}: {base / 20 * 1e3:.1f} us, shifted by {shift:.0f} {shifted / 20 * 1e3:.1f} us")
+        assert shifted <= 2.5 * base, (dtype, M, V, base, shifted)
