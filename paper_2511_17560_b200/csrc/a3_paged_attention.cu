@@ -336,7 +336,7 @@ paged_attention_kernel(const PagedAttnArgs a) {
 
     // Three steps of a tile, each in its own turn: its pages are looked up, three turns later its rows are copied, two turns after that it
     // is computed.  Pages and rows come by asynchronous copies, so that no turn waits for an access that it makes itself.
-    int xs = seq0, xn = len0, xt = (int)(w0 - first0), xp = xt * KT / a.page_size, xe = xt * KT - xp * a.page_size;
+    int xs = seq0, xn = len0, xt = (int)min(w0 - first0, (unsigned)cap / KT), xp = xt * KT / a.page_size, xe = xt * KT - xp * a.page_size;
     // lengths of the 32 sequences behind the first one, of the 32 behind those once they are done with, a lane for each
     int x_left = count, x_base = xs + 1, x_len = 0;
     auto lengths = [&] { x_len = x_base + lane < a.n_seqs ? length(x_base + lane) : 0; };
@@ -482,7 +482,7 @@ paged_attention_kernel(const PagedAttnArgs a) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[mt][nt][e] = 0.f;
         }
-        if (NT == 1 && count - i > (cn + KT - 1) / KT - ct) {  // more sequences follow: of the next one, unless it is empty
+        if (NT == 1 && cs + 1 < a.n_seqs && count - i > (cn + KT - 1) / KT - ct) {  // more sequences follow: of the next one, unless it is empty
           ++q_seq;
           load_q();
         }

@@ -34,3 +34,60 @@ def test_launches_that_others_run_beside_are_ordinary():
     for call in re.findall(r"enter_rows\([^;]*;", source("a3_api.cu")):
         last = call.rsplit(",", 1)[1].strip(" \n);")
         assert last in ("st", "recovering", "i == 0 && recovering"), last
+
+
+def test_lengths_that_change_under_the_call_lead_nowhere():
+    """paged_attention_kernel reads each length several times, and promises bounds even where another stream writes them meanwhile.  A warp's walk over its
+    tiles, with the lengths of the scan and others read later; a rule that the source lacks is left out here too."""
+    import itertools
+    import random
+
+    text = source("a3_paged_attention.cu")
+    next_there = bool(re.search(r"if \(NT == 1 && cs \+ 1 < a\.n_seqs && count - i >", text))
+    clamped = bool(re.search(r"xt = \(int\)min\(w0 - first0, \(unsigned\)cap / KT\)", text))
+
+    def walk(scan, later, first_seq, skip, KT, cap):
+        """Sequences whose queries are read, and the keys that tiles begin with."""
+        tiles = lambda n: -(-n // KT)  # noqa: E731
+        n_seqs, queries, keys = len(scan), [first_seq], []
+        count = sum(tiles(x) for x in scan[first_seq:]) - skip
+        xs, xn, xt = first_seq, scan[first_seq], min(skip, cap // KT) if clamped else skip
+        q_seq, fresh = first_seq, True
+        for i in range(count):
+            cs, cn, ct = xs, xn, xt
+            keys.append(ct * KT)
+            if fresh:
+                fresh = False
+                if q_seq != cs:
+                    q_seq = cs
+                    queries.append(q_seq)
+                if count - i > tiles(cn) - ct and (cs + 1 < n_seqs or not next_there):
+                    q_seq += 1
+                    queries.append(q_seq)
+            fresh |= ct == tiles(cn) - 1
+            xt += 1
+            if xt * KT >= xn:
+                xt = 0
+                while True:
+                    if xs == n_seqs - 1:
+                        xn = 0
+                        break
+                    xs += 1
+                    xn = later[xs]
+                    if xn > 0:
+                        break
+        return queries, keys
+
+    rng = random.Random(0)
+    for scan, later in itertools.product(itertools.product((0, 1, 16, 33, 64), repeat=3), repeat=2):
+        if scan[0]:
+            queries, keys = walk(scan, later, 0, 0, 16, 64)
+            assert all(0 <= q < 3 for q in queries) and all(k <= 64 + 16 for k in keys), (scan, later, queries)
+    for _ in range(500):
+        cap = rng.choice((64, 2 ** 31 - 2 ** 16))
+        scan, later = [[rng.choice((0, 1, 16, 500)) % (cap + 1) for _ in range(6)] for _ in range(2)]
+        # a stretch whose first sequence and first tile were written by two threads that saw different lengths
+        queries, keys = walk(scan, later, rng.randrange(6), rng.choice((0, 1, 3, 2 ** 28)), 16, cap)
+        assert all(0 <= q < 6 for q in queries) and all(k <= cap + 16 for k in keys)
+    # the first tile of a stretch far along a line of 2^34 slots: its first key has to fit 32 bits
+    assert clamped
