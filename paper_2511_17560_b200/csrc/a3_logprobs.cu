@@ -196,8 +196,14 @@ __device__ __forceinline__ uint32_t cluster_rank() {
   asm("mov.u32 %0, %cluster_ctarank;" : "=r"(x));
   return x;
 }
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive() {
+  __syncwarp();  // a warp's lanes arrive, and wait, as one, wherever a loop before has left them
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+  __syncwarp();
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 template <typename V>
 __device__ __forceinline__ V* in_first(V* p, int parts) {
   if (parts == 1) return p;

@@ -141,6 +141,7 @@ __device__ __forceinline__ const V* of_rank(const V* p, unsigned rank) {
   return q;
 }
 __device__ __forceinline__ void cluster_sync() {
+  __syncwarp();  // a warp's lanes arrive as one, wherever a loop before has left them
   asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // Two bf16, neither above its number (of numbers from 0 on).

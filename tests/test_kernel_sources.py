@@ -91,3 +91,11 @@ def test_lengths_that_change_under_the_call_lead_nowhere():
         assert all(0 <= q < 6 for q in queries) and all(k <= cap + 16 for k in keys)
     # the first tile of a stretch far along a line of 2^34 slots: its first key has to fit 32 bits
     assert clamped
+
+
+def test_lanes_meet_before_a_barrier_of_a_cluster():
+    """The aligned forms of the cluster barrier want a warp's lanes together, and both kernels reach it from loops that lanes leave at different times."""
+    for name in ("a3_paged_attention.cu", "a3_logprobs.cu"):
+        text = source(name)
+        barriers = [m.start() for m in re.finditer(r"asm volatile\(\"barrier\.cluster\.(arrive|wait)", text)]
+        assert barriers and all(re.search(r"__syncwarp\(\);\s*$", text[:at]) for at in barriers), name
