@@ -16,7 +16,7 @@ import torch
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "liba3.so")
 _lib = None
-_calls = None  # csrc/a3_calls.cpp, and the addresses of the library's functions that it calls
+_calls = None  # csrc/a3_calls.cpp, from the first decoding call on, and the addresses of the library's functions that it calls
 _entry: Dict[str, int] = {}
 
 A3_OK = 0
@@ -95,17 +95,12 @@ class LayerPlan(C.Structure):
 
 
 def _load():
-    global _lib, _calls
+    global _lib
     if _lib is not None:
         return _lib
     if not os.path.exists(_LIB_PATH):
         raise ImportError(f"{_LIB_PATH} is missing: build it with `python -m paper_2511_17560_b200.build` "
                           "(there is no fallback path)")
-    try:
-        from . import a3_calls
-    except ImportError as e:
-        raise ImportError("a3_calls is missing or made for another torch: build it with `python -m paper_2511_17560_b200.build` "
-                          "(there is no fallback path)") from e
     lib = C.CDLL(_LIB_PATH)
     vp, i32, u64, sz = C.c_void_p, C.c_int, C.c_uint64, C.c_size_t
     lib.a3_create.argtypes = [C.POINTER(vp), C.POINTER(ModelDesc), C.POINTER(LayerWeights)]
@@ -160,11 +155,27 @@ def _load():
     lib.a3_kernel_class_name.argtypes = [i32]
     lib.a3_kernel_class_name.restype = C.c_char_p
     lib.a3_plan_layer.argtypes = [C.POINTER(ModelDesc), i32, i32, C.POINTER(LayerPlan)]
-    a3_calls.set_error(A3Error)
     for name in ("a3_paged_append", "a3_paged_attention_workspace_bytes", "a3_paged_attention", "a3_token_logprobs"):
         _entry[name] = C.cast(getattr(lib, name), vp).value
-    _lib, _calls = lib, a3_calls
+    _lib = lib
     return lib
+
+
+def _decoding():
+    """The compiled part of the binding.  It is made for one torch, and the decoding calls alone need it: the rest of the binding does without."""
+    global _calls
+    if _calls is None:
+        _load()
+        build = "build it with `python -m paper_2511_17560_b200.build` (there is no fallback path)"
+        try:
+            from . import a3_calls
+        except ImportError as e:
+            raise ImportError(f"a3_calls is missing or made for another torch: {build}") from e
+        if a3_calls.torch_version != str(torch.__version__):
+            raise ImportError(f"a3_calls is made for torch {a3_calls.torch_version}, this is {torch.__version__}: {build}")
+        a3_calls.set_error(A3Error)
+        _calls = a3_calls
+    return _calls
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -460,21 +471,21 @@ class A3:
     def paged_append(self, cache: PagedCache, page_table, row_seq, row_slot, k_rows, v_rows, q_rows=None, row_pos=None, rotate=True, q_out=None):
         """a3_paged_append; page_table [n_seqs][max_pages], rows [M][heads][D] (columns of a wider buffer will do); returns q_out or None."""
         m = self.shape
-        return _calls.paged_append(_entry["a3_paged_append"], self._h.value, self._on(cache, "a3_paged_append"), _stream(), self.device,
+        return (_calls or _decoding()).paged_append(_entry["a3_paged_append"], self._h.value, self._on(cache, "a3_paged_append"), _stream(), self.device,
                                    m.n_q_heads, m.n_kv_heads, m.head_dim, page_table, row_seq, row_slot, k_rows, v_rows, q_rows, row_pos, rotate, q_out)
 
     def paged_attention(self, cache: PagedCache, page_table, cache_len, q_rows, scale=None, out=None, want_lse=False):
         """a3_paged_attention; returns (out [n_seqs][Hq][D], lse [n_seqs][Hq] or None).  The workspace is allocated by torch for
         this call alone, so that calls on several streams, or captured into several graphs, share none."""
         m = self.shape
-        return _calls.paged_attention(_entry["a3_paged_attention"], _entry["a3_paged_attention_workspace_bytes"], self._h.value,
+        return (_calls or _decoding()).paged_attention(_entry["a3_paged_attention"], _entry["a3_paged_attention_workspace_bytes"], self._h.value,
                                       self._on(cache, "a3_paged_attention"), _stream(), self.device, m.n_q_heads, m.head_dim, page_table, cache_len, q_rows,
                                       m.head_dim ** -0.5 if scale is None else scale, out, want_lse)
 
     def token_logprobs(self, logits, targets=None, n_top=0):
         """a3_token_logprobs on logits [M][vocab] (fp32, bf16 or fp16; rows may be apart); returns (logprob [M] or None without targets,
         entropy [M], top_ids [M][n_top] and top_logprobs [M][n_top], or None)."""
-        return _calls.token_logprobs(_entry["a3_token_logprobs"], self._h.value, _stream(), self.device, logits, targets, n_top)
+        return (_calls or _decoding()).token_logprobs(_entry["a3_token_logprobs"], self._h.value, _stream(), self.device, logits, targets, n_top)
 
     def make_request(self, chunks, n_chunks, max_chunk_len, n_ctx, n_question, x0, k_fused, v_fused, ratio=0.15,
                      select_layer=1, n_system=0, forced_re=None, n_recompute=None, score_source=0, evict_capacity=0,

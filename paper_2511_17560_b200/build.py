@@ -15,6 +15,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "liba3.so")
 CALLS = os.path.join(PKG, "a3_calls.so")
+CALLS_FOR = os.path.join(PKG, "build", "a3_calls.torch")  # the version of torch that it was made for
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
          "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
@@ -31,20 +32,36 @@ def _stale(target, deps):
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def calls_stale() -> bool:
+    """Whether a3_calls.so is missing, older than its sources, or made for another torch than the one that is installed."""
+    import torch
+
+    if _stale(CALLS, [os.path.join(CSRC, "a3_calls.cpp"), os.path.join(ROOT, "include", "a3.h"), os.path.join(os.path.dirname(torch.__file__), "version.py")]):
+        return True
+    if not os.path.exists(CALLS_FOR):
+        return True
+    with open(CALLS_FOR) as f:
+        return f.read() != str(torch.__version__)
+
+
 def build_calls(force: bool = False) -> str:
     """a3_calls.so, against the headers and libraries of the torch that is installed."""
     import torch
 
     src, base = os.path.join(CSRC, "a3_calls.cpp"), os.path.dirname(torch.__file__)
-    if force or _stale(CALLS, [src, os.path.join(ROOT, "include", "a3.h"), os.path.join(base, "version.py")]):
+    if force or calls_stale():
         inc = [os.path.join(base, "include"), os.path.join(base, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"]]
         cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+               f'-DA3_TORCH_VERSION="{torch.__version__}"',
                "-I", os.path.join(ROOT, "include")] + [a for i in inc for a in ("-isystem", i)]
         cmd += [src, "-o", CALLS, "-L", os.path.join(base, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"]
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode:
             sys.stderr.write(r.stdout + r.stderr)
             raise RuntimeError("g++ failed for " + src)
+        os.makedirs(os.path.dirname(CALLS_FOR), exist_ok=True)
+        with open(CALLS_FOR, "w") as f:
+            f.write(str(torch.__version__))
     return CALLS
 
 

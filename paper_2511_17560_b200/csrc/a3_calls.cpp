@@ -221,4 +221,9 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "a3_calls", nullptr, -1, methods, n
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit_a3_calls() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit_a3_calls() {
+  PyObject* m = PyModule_Create(&module);
+  // tensors are looked at through torch's own classes: of another version even what links may lie elsewhere
+  if (m && PyModule_AddStringConstant(m, "torch_version", A3_TORCH_VERSION) < 0) Py_CLEAR(m);
+  return m;
+}

@@ -207,3 +207,40 @@ def test_null_handles():
     assert lib.a3_paged_append(None, None, None, None) == -1
     assert lib.a3_paged_attention(None, None, None, None) == -1
     assert lib.a3_token_logprobs(None, None, None) == -1
+
+
+@pytest.mark.parametrize("spoil,message", [("sys.modules['paper_2511_17560_b200.a3_calls'] = None", "missing or made for another torch"),
+                                           ("torch.__version__ = '2.0.0+other'", "is made for torch")])
+def test_the_rest_of_the_binding_needs_no_compiled_calls(spoil, message):
+    """Without a3_calls.so, or with one made for another torch, everything but the decoding calls works; those say what is wrong."""
+    code = f"""
+import sys
+import torch
+{spoil}
+from paper_2511_17560_b200 import a3
+assert a3.recompute_count(0.5, 10, 10) > 0 and a3.launch_count() == 0
+e = a3.A3.__new__(a3.A3)
+e._h, e.device, e._ws = a3.C.c_void_p(), torch.device("cpu"), None
+for _ in range(2):
+    try:
+        e.token_logprobs(torch.zeros((3, 80)))
+    except ImportError as error:
+        assert {message!r} in str(error) and "paper_2511_17560_b200.build" in str(error), error
+    else:
+        raise AssertionError("no ImportError")
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    subprocess.run([sys.executable, "-c", code], cwd=root, check=True)
+
+
+def test_compiled_calls_are_made_anew_for_another_torch(monkeypatch, tmp_path):
+    from paper_2511_17560_b200 import build
+
+    stamp = tmp_path / "torch"
+    monkeypatch.setattr(build, "CALLS_FOR", str(stamp))
+    monkeypatch.setattr(build, "_stale", lambda target, deps: False)
+    assert build.calls_stale()
+    stamp.write_text(str(torch.__version__))
+    assert not build.calls_stale()
+    monkeypatch.setattr(torch, "__version__", "2.0.0+other")
+    assert build.calls_stale()
