@@ -290,10 +290,11 @@ class PagedCache:
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
                  v_scale: Optional[torch.Tensor] = None):
         where = "PagedCache"
-        _need(k_pages.dim() == 4 and k_pages.shape == v_pages.shape and k_pages.stride() == v_pages.stride()
-              and k_pages.dtype == v_pages.dtype and k_pages.device == v_pages.device and min(k_pages.shape) > 0, where + " pages")
+        _need(k_pages.dim() == 4 and k_pages.shape == v_pages.shape and k_pages.dtype == v_pages.dtype and k_pages.device == v_pages.device
+              and min(k_pages.shape) > 0, where + " pages")
         n, size, heads, d = k_pages.shape
-        _need(k_pages.stride()[1:] == (heads * d, d, 1), where + " pages are contiguous")
+        _need(all(t[0].is_contiguous() for t in (k_pages, v_pages)), where + " pages are contiguous")
+        _need(n == 1 or k_pages.stride(0) == v_pages.stride(0), where + " pages are as far apart in both pools")
         _need(k_pages.dtype in (torch.bfloat16, torch.float8_e4m3fn), where + " type")
         packed = k_pages.dtype == torch.float8_e4m3fn
         for s in (k_scale, v_scale):

@@ -244,3 +244,18 @@ def test_compiled_calls_are_made_anew_for_another_torch(monkeypatch, tmp_path):
     assert not build.calls_stale()
     monkeypatch.setattr(torch, "__version__", "2.0.0+other")
     assert build.calls_stale()
+
+
+def test_cache_of_single_pages_entries_and_heads():
+    """Where there is one page, one entry or one KV head, the stride of that dimension says nothing about where elements lie."""
+    bf = torch.bfloat16
+    one_head = torch.zeros((3, 1, 16, 64), dtype=bf).transpose(1, 2)  # [3][16][1][64]
+    assert one_head.stride() == (1024, 64, 1024, 1)
+    c = a3.PagedCache(one_head, pages(heads=1))
+    assert (c.desc.page_stride, c.n_kv_heads, c.page_size) == (16 * 64 * 2, 1, 16)
+    one_entry = torch.zeros((3, 2, 1, 64), dtype=bf).transpose(1, 2)  # [3][1][2][64]
+    assert a3.PagedCache(one_entry, pages(size=1)).desc.page_stride == 2 * 64 * 2
+    apart = torch.zeros((4, 2, 16, 2, 64), dtype=bf)
+    assert a3.PagedCache(apart[:1, 0], pages(n=1)).desc.page_stride == 16 * 2 * 64 * 2  # no second page to be apart from
+    for k, v in [(apart[:, 0], pages(n=4)), (pages().transpose(1, 2).contiguous().transpose(1, 2), pages())]:
+        refused(a3.PagedCache, k, v)
