@@ -193,7 +193,7 @@ PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
       logprob = at::empty({M}, fp32);
       r.targets = (const int32_t*)targets->data_ptr(), r.logprob_out = (float*)logprob.data_ptr();
     }
-    if (n_top > 0) {
+    if (n_top > 0 && n_top <= A3_LOGPROBS_MAX_TOP) {  // the library refuses more
       ids = at::empty({M, n_top}, x.options().dtype(at::kInt));
       lps = at::empty({M, n_top}, fp32);
       r.top_ids_out = (int32_t*)ids.data_ptr(), r.top_logprobs_out = (float*)lps.data_ptr();

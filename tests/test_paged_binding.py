@@ -259,3 +259,20 @@ def test_cache_of_single_pages_entries_and_heads():
     assert a3.PagedCache(apart[:1, 0], pages(n=1)).desc.page_stride == 16 * 2 * 64 * 2  # no second page to be apart from
     for k, v in [(apart[:, 0], pages(n=4)), (pages().transpose(1, 2).contiguous().transpose(1, 2), pages())]:
         refused(a3.PagedCache, k, v)
+
+
+def test_more_alternatives_than_there_can_be_are_refused_before_anything_is_allocated(eng, monkeypatch):
+    """n_top beyond what the library takes goes to the library, whose status it is, without results of that size."""
+    given = []
+
+    def refuses(h, fields, stream):
+        given.append(R.LOGIT_ROWS.unpack(ctypes.string_at(fields, R.LOGIT_ROWS.size)))
+        return -2
+
+    f = ctypes.CFUNCTYPE(ctypes.c_int, *[ctypes.c_void_p] * 3)(refuses)
+    monkeypatch.setitem(a3._entry, "a3_token_logprobs", ctypes.cast(f, ctypes.c_void_p).value)
+    x = torch.zeros((4096, 8))
+    for n in (33, (1 << 31) - 1):  # 2^43 elements
+        with pytest.raises(a3.A3Error) as e:
+            eng.token_logprobs(x, None, n)
+        assert e.value.status == -2 and given[-1][-1] == n and given[-1][4:6] == (0, 0)
