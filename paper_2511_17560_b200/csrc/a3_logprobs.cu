@@ -428,7 +428,7 @@ logprobs_kernel(const LogprobArgs a) {
   auto again = [&](int t, auto use) {
     for (int v = v0 + t + lane * THREADS; v < v1; v += 32 * THREADS) {
       float f[VE];
-      Logit<T>::unpack(__ldg(xv + v), f);
+      Logit<T>::unpack(__ldcg(xv + v), f);
 #pragma unroll
       for (int e = 0; e < VE; ++e) use(f[e], head + v * VE + e);
     }
@@ -487,7 +487,7 @@ logprobs_kernel(const LogprobArgs a) {
           for (int q = 0; q < 4; ++q) {
             const int at = i + q * WARPS;
             v[q] = at < found ? v0 + k + s_found[at] : v1;
-            if (v[q] < v1) raw[q] = __ldg(xv + v[q]);
+            if (v[q] < v1) raw[q] = __ldcg(xv + v[q]);
           }
 #pragma unroll
           for (int q = 0; q < 4; ++q) {

@@ -90,7 +90,7 @@ paged_append_kernel(const AppendArgs a) {
         const bf16* src = (h < a.q_heads ? q : h < a.q_heads + a.kv_heads ? k : v) + h * D;
         x[i][0] = __ldcs(reinterpret_cast<const uint4*>(src));
         x[i][1] = __ldcs(reinterpret_cast<const uint4*>(src + D / 2));
-        if (F8 && h >= a.q_heads) scale[i] = __ldg(h < a.q_heads + a.kv_heads ? a.k_scale + (h - a.q_heads) : a.v_scale + (h - a.q_heads - a.kv_heads));
+        if (F8 && h >= a.q_heads) scale[i] = __ldca(h < a.q_heads + a.kv_heads ? a.k_scale + (h - a.q_heads) : a.v_scale + (h - a.q_heads - a.kv_heads));
       }
     }
     const bool turned = a.rotate && pos < 0, live = page != -2;

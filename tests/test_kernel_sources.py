@@ -99,3 +99,11 @@ def test_lanes_meet_before_a_barrier_of_a_cluster():
         text = source(name)
         barriers = [m.start() for m in re.finditer(r"asm volatile\(\"barrier\.cluster\.(arrive|wait)", text)]
         assert barriers and all(re.search(r"__syncwarp\(\);\s*$", text[:at]) for at in barriers), name
+
+
+def test_decoding_reads_nothing_as_read_only_that_the_launch_before_may_write():
+    """These kernels begin while the launch before them may still run.  A read-only load says that nobody writes during the kernel, and may be moved in front
+    of the wait: it is for the table of angles, which is written when a handle is made."""
+    for name in ("a3_paged_append.cu", "a3_paged_attention.cu", "a3_logprobs.cu"):
+        loads = re.findall(r"(?:__ldg|ld\.global\.nc)\S*", source(name))
+        assert all(x.startswith("__ldg(tr") for x in loads), (name, loads)
