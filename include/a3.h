@@ -475,7 +475,8 @@ int a3_plan_layer(const a3_model_desc* model, int sm_count, int rows, a3_layer_p
  * a3_profile_read waits for `stream`, adds up the elapsed time per class and clears the records. */
 typedef enum {
   A3_K_REROTATE = 0, A3_K_RMSNORM, A3_K_GEMM_QKV, A3_K_ATTENTION, A3_K_GEMM_RESIDUAL, A3_K_GEMM_SWIGLU,
-  A3_K_SCORES, A3_K_TOPK, A3_K_ROWS /* gather, scatter, index kernels */, A3_K_FIRST_TOKEN, A3_K_CLASSES
+  A3_K_SCORES, A3_K_TOPK, A3_K_ROWS /* gather, scatter, index kernels */, A3_K_FIRST_TOKEN,
+  A3_K_PAGED_APPEND, A3_K_PAGED_ATTENTION /* and its join */, A3_K_TOKEN_LOGPROBS, A3_K_CLASSES
 } a3_kernel_class;
 typedef struct { uint64_t launches; double ms; } a3_profile_entry;
 int a3_profile_enable(a3_handle* h, int max_records);

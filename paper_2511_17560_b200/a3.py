@@ -83,7 +83,7 @@ EXPORTS = ("a3_create", "a3_destroy", "a3_set_option", "a3_scores_workspace_byte
            "a3_graph_capture", "a3_graph_launch", "a3_graph_kernel_count", "a3_graph_destroy",
            "a3_device_status", "a3_status_string", "a3_last_cuda_error", "a3_launch_count", "a3_profile_enable",
            "a3_profile_read", "a3_kernel_class_name", "a3_plan_layer")
-K_CLASSES = 10
+K_CLASSES = 13
 
 
 class ProfileEntry(C.Structure):

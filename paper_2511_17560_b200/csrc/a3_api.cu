@@ -266,7 +266,8 @@ extern "C" int a3_profile_read(a3_handle* h, a3_profile_entry* out, a3_stream st
 
 extern "C" const char* a3_kernel_class_name(int cls) {
   static const char* names[A3_K_CLASSES] = {"rerotate", "rmsnorm", "gemm_qkv", "attention", "gemm_residual",
-                                            "gemm_swiglu", "scores", "topk", "rows", "first_token"};
+                                            "gemm_swiglu", "scores", "topk", "rows", "first_token",
+                                            "paged_append", "paged_attention", "token_logprobs"};
   return cls >= 0 && cls < A3_K_CLASSES ? names[cls] : "?";
 }
 

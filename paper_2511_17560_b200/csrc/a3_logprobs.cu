@@ -684,7 +684,7 @@ extern "C" int a3_token_logprobs(const a3_handle* h, const a3_logit_rows* rows, 
   if ((p.M > 1 && p.row_stride < (uint64_t)p.vocab) || p.row_stride > (uint64_t)1 << 31) return A3_EINVAL;
   const LogprobArgs a{p.logits, (long long)p.row_stride, p.M, p.vocab, p.targets, p.n_top, p.logprob_out, p.entropy_out, p.top_ids_out, p.top_logprobs_out, h->dev_status};
   cudaStream_t st = (cudaStream_t)stream;
-  ProfScope prof(h, A3_K_FIRST_TOKEN, st);
+  ProfScope prof(h, A3_K_TOKEN_LOGPROBS, st);
   return p.type == A3_LOGITS_FP32 ? logprobs_launch<float>(h, a, st) : p.type == A3_LOGITS_BF16 ? logprobs_launch<bf16>(h, a, st)
                                                                                                 : logprobs_launch<__half>(h, a, st);
 }

@@ -205,7 +205,7 @@ extern "C" int a3_paged_append(const a3_handle* h, const a3_paged_cache* cache, 
   const unsigned long long need = ((unsigned long long)p.M * cdiv(all, heads) * uph + PA_THREADS - 1) / PA_THREADS;
   const unsigned blocks = (unsigned)(need < (unsigned long long)h->sm_count * PA_MIN ? need : (unsigned long long)h->sm_count * PA_MIN);
   cudaStream_t st = (cudaStream_t)stream;
-  ProfScope prof(h, A3_K_ROWS, st);
+  ProfScope prof(h, A3_K_PAGED_APPEND, st);
   const bool f8 = cache->type == A3_CACHE_E4M3;
   auto go = [&](auto one, auto four) { return launch_pdl(many ? four : one, dim3(blocks), dim3(PA_THREADS), 0, st, a); };
   auto pick = [&](auto d, auto layout) {

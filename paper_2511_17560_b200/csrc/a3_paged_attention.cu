@@ -921,10 +921,14 @@ static int paged_launch(const a3_handle* h, const PagedAttnArgs& a, int units, c
   static SmemAttrOnce once;
   using C = PagedCfg<D, F8, NT>;
   A3_TRY(smem_attr_once(once, h->device, paged_attention_kernel<D, F8, NT, WHOLE>, C::SMEM));
-  A3_CUDA(launch_pdl_cluster(a.by_seq > 1 ? a.by_seq : 1, paged_attention_kernel<D, F8, NT, WHOLE>, dim3((a.by_seq ? a.n_seqs * a.by_seq : a.most_parts) * units),
-                             dim3(C::THREADS), C::SMEM, st, a));
-  A3_LAUNCHED();
+  {
+    ProfScope prof(h, A3_K_PAGED_ATTENTION, st);
+    A3_CUDA(launch_pdl_cluster(a.by_seq > 1 ? a.by_seq : 1, paged_attention_kernel<D, F8, NT, WHOLE>, dim3((a.by_seq ? a.n_seqs * a.by_seq : a.most_parts) * units),
+                               dim3(C::THREADS), C::SMEM, st, a));
+    A3_LAUNCHED();
+  }
   if (a.by_seq || a.most_parts == 1) return A3_OK;  // every sequence ends in the part that it begins in
+  ProfScope prof(h, A3_K_PAGED_ATTENTION, st);
   A3_CUDA(launch_pdl(paged_join_kernel<D>, dim3(a.most_parts - 1, units, a.unit), dim3(32 * PJ_WARPS), a.most_parts * sizeof(float), st, a));
   return launched();
 }
@@ -977,7 +981,6 @@ extern "C" int a3_paged_attention(const a3_handle* h, const a3_paged_cache* cach
   a.status = h->dev_status;
   cudaStream_t st = (cudaStream_t)stream;
   const int units = m.n_kv_heads * plan.groups;
-  ProfScope prof(h, A3_K_ATTENTION, st);
   const bool f8 = cache->type == A3_CACHE_E4M3;
   auto heads = [&](auto d, auto nt) {
     constexpr int DD = decltype(d)::value, N = decltype(nt)::value;

@@ -106,3 +106,12 @@ def test_host_only_helpers_match_oracle():
     for ratio, n, nc in ((0.15, 5152, 5120), (1.0, 100, 90), (0.0, 10, 10), (0.3, 10, 2), (0.15, 20, 20)):
         assert a3.recompute_count(ratio, n, nc) == O.recompute_count(ratio, n, nc)
     assert a3.evict_count(1024, 40, 5120, 32) == 952 and a3.evict_count(10, 40, 5120, 32) == 0 and a3.evict_count(10**6, 0, 100, 5) == 100
+
+
+def test_kernel_classes_are_all_named(lib_path):
+    """The binding reads as many records as the library writes, each under a name of its own."""
+    from paper_2511_17560_b200 import a3
+    lib = a3._load()
+    names = [lib.a3_kernel_class_name(k) for k in range(a3.K_CLASSES)]
+    assert b"?" not in names and len(set(names)) == a3.K_CLASSES and lib.a3_kernel_class_name(a3.K_CLASSES) == b"?"
+    assert {b"paged_append", b"paged_attention", b"token_logprobs"} <= set(names)

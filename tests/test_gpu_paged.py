@@ -528,6 +528,26 @@ def test_attention_of_infinite_values(a3, lens):
     check_attention(a3, eng, cache, table, lens, q)
 
 
+def test_profiles_tell_decoding_from_fusion(a3):
+    """Each of the decoding calls is a class of its own, with a record for every launch."""
+    hq, hkv, d = SHAPES["g2"]
+    m = replace(W.TINY, n_layers=1, n_q_heads=hq, n_kv_heads=hkv, head_dim=d, d_model=128, d_ff=128)
+    eng, g = a3.A3(m, W.make_weights_device(m, torch.device(DEV), 0), 64), gen(32)
+    kp, vp, _, _ = make_pool(g, 4, 16, hkv, d, False)
+    cache, q, k = a3.PagedCache(kp, vp), randn(g, 1, hq, d), randn(g, 1, hkv, d)
+    narrow, wide = ints([[1, 2]]), ints([[1] * 4000])
+    eng.profile_enable(64)
+    a3.launch_count(reset=True)
+    eng.paged_append(cache, narrow, ints([0]), ints([3]), k, k, q_rows=q)
+    eng.paged_attention(cache, narrow, ints([4]), q)
+    eng.paged_attention(cache, wide, ints([4]), q)  # two launches
+    eng.token_logprobs(torch.zeros((2, 100), device=DEV))
+    got = {name: e["launches"] for name, e in eng.profile_read().items() if e["launches"]}
+    assert got == {"paged_append": 1, "paged_attention": 3, "token_logprobs": 1} and a3.launch_count() == 5
+    eng.profile_enable(0)
+    eng.close()
+
+
 # ------------------------------------------------------------------ refusals
 
 
