@@ -407,7 +407,8 @@ int a3_paged_append(const a3_handle* h, const a3_paged_cache* cache, const a3_pa
  * with q_rows rotated and the new token's own slot counted in cache_len.  A sequence of length 0 (padding of a batch of fixed size)
  * gives zeros and -inf.  A length below 0 or above max_pages*page_size counts as 0, keys and values of a page outside [0, n_pages) count
  * as zeros, and both set A3_DEV_BAD_POSITION.  A3_ETOOLARGE: max_pages*page_size above 2^31 - 2^16, or n_seqs times that above
- * 2^34.  Lengths are read on the device only, so a captured call follows them.  The result is deterministic.
+ * 2^34.  Lengths are read on the device only, so a captured call follows them.  The result is deterministic; how the
+ * keys are divided, and with it the last bits, depends on the lengths, max_pages, page_size, n_seqs and the device.
  * The workspace is borrowed until the call's kernels have ended and needs no clearing.  At most two launches, no allocation, no
  * synchronisation. */
 typedef struct {

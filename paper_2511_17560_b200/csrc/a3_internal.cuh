@@ -91,6 +91,7 @@ struct ProfScope {
 // successor do the same with pdl_launch_dependents().  Both instructions are no-ops under an ordinary launch.
 // Exceptions, which read and write before they wait (and wait before they end):
 //   * the pair GEMMs' first weights, which no launch writes;
+//   * paged_attention_kernel's prefetches into L2, which read nothing;
 //   * first_token_kernel behind clear_ticket_kernel, and enter_rows_kernel with `beside` behind rerotate_kernel.  Those two
 //     predecessors start with an early trigger, touch nothing that the kernel beside them touches before its wait, and are ORDINARY
 //     launches: what was queued before them has ended.  They must not become programmatic ones, and nothing may be queued between.

@@ -14,9 +14,10 @@
 // through again, in the ring where that still holds the row, else from L2, a warp together on one thread's elements.  What reaches the
 // bound, usually 1-2 n elements, is ranked by counting.
 //
-// Measured, bf16: 2 048 rows of 128 256, 525 MB, one alternative each, 87 us while the clock holds (6.0 TB/s) and 96-103 us repeated without a pause,
-// when the power limit lowers it to 1.6 GHz: an exponential and some seven other instructions for each element fill the SM as the way from HBM does.  65 rows
-// of 152 064 with 20 alternatives each 12.6 us, one row of 128 256 in fp32 7.4 us: latency, the ranking after the pass among it.
+// Measured, bf16: 2 048 rows of 128 256, 525 MB, one alternative each, 87 us while the clock holds (6.0 TB/s) and 102-105 us repeated without a pause,
+// when the power limit lowers it to 1.6 GHz: an exponential and some seven other instructions for each element fill the SM as the way from HBM does; with 20
+// alternatives 129 us, the search and the ranking of a row with no load under way.  65 rows of 152 064 with 20 alternatives each 12.4 us, one row of
+// 128 256 in fp32 7.2 us: latency, the ranking after the pass among it.  With a nearly certain token in every row 13.0, 7.6 and 89 us.
 #include <cuda_fp16.h>
 
 #include "a3_internal.cuh"
@@ -654,13 +655,14 @@ static int logprobs_rows(const a3_handle* h, const LogprobArgs& a, int parts, cu
 
 template <typename T>
 static int logprobs_launch(const a3_handle* h, const LogprobArgs& a, cudaStream_t st) {
-  // CTAs of a row: up to two for each SM (65 rows of 152 064 in bf16, of which 20 each: 4 CTAs a row 13.1 us, 8 17.2), no fewer than 2 048
+  // CTAs of a row: up to two for each SM (65 rows of 152 064 in bf16, of which 20 each: 4 CTAs a row 12.4 us, 8 16.5), no fewer than 2 048
   // elements for each.
   int parts = 1;
   while (parts < LP_PARTS && (long long)a.M * parts * 2 <= 2 * h->sm_count && a.vocab / (2 * parts) >= 2048) parts *= 2;
   if (parts > 1) return logprobs_rows<T, 256, LP_PARTS>(h, a, parts, st);
-  // Short rows in small CTAs, of which more are at work at once: 858 rows of 21 870 in fp16 14.1 us with 64 threads, 16.0 with 128 and 20.6 with
-  // 256; 2 500 of 32 000 in bf16 69, 53 and 56; 1 000 of 128 256 in fp32 167, 119 and 96.
+  // Short rows in small CTAs, of which more are at work at once.  With 64, 128 and 256 threads and 5 alternatives: 858 rows of 21 870 in fp16 14.7 us, 14.8
+  // and 19.8; 2 500 of 24 000 in bf16 37.9, 33.6 and 42.2, of 32 000 48.1, 39.2 and 42.7; 1 500 of 48 000 43.7, 36.0 and 35.8, of 65 536 61.1, 47.0
+  // and 42.6; 1 000 of 128 256 in fp32 144, 114 and 94.  The lines could lie a little lower, near 44 and 96 KiB.
   const long long bytes = (long long)a.vocab * sizeof(T);
   if (bytes <= 52 << 10) return logprobs_rows<T, 64, 1>(h, a, 1, st);
   if (bytes <= 128 << 10) return logprobs_rows<T, 128, 1>(h, a, 1, st);

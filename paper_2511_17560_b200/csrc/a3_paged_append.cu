@@ -6,7 +6,7 @@
 //
 // Bound by HBM where rows are many, by latency where they are few.  Measured on heads of 128: 17 871 rows of 28 heads over 4, bf16, 342 MB, in
 // 57.5 us, 5.9 TB/s; 32 768 rows of 8 KV heads into 8 bits, 202 MB, in 39.5 us, 5.1 TB/s (rotation and conversion issue for half of
-// the time); 256 rows of a batch 2.6 us, one row 1.8 us.
+// the time); 256 rows of a batch 2.4 us, one row 1.7 us.
 #include <cuda_fp8.h>
 
 #include "a3_internal.cuh"

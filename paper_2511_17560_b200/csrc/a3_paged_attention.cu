@@ -15,9 +15,9 @@
 // unnormalised output) and a second kernel merges it in the order of the keys.  The division depends on the lengths and
 // the device only: results do not depend on timing.
 //
-// Measured, 32 query heads over 8 of 128, bf16: 128 sequences of up to 8 191 slots, 2.0 GB, in 300 us, 6.7 TB/s, as fast as a copy; one of 5 153 slots,
+// Measured, 32 query heads over 8 of 128, bf16: 128 sequences of up to 8 191 slots, 2.0 GB, in 298-312 us, 6.4-6.7 TB/s, as fast as a copy; one of 5 153 slots,
 // 21 MB, in 10.2 us by eight CTAs for each KV head, nearly all of them lengths, pages and keys one after the other and the two merges; where a
-// second launch joins, that is 2 us more; one of 32 801 in 8 bits, 67 MB, in 20.9 us.  28 heads over 4, 8 bits, 16 sequences of up to 15 675 slots, 157 MB, in 35.5 us: the
+// second launch joins, that is 2 us more; one of 32 801 in 8 bits, 67 MB, in 21.3-21.9 us.  28 heads over 4, 8 bits, 16 sequences of up to 15 675 slots, 157 MB, in 34.3-36.3 us: the
 // widening and the products of 8-bit tiles take as long as their way from HBM, and the SM with the slowest way to it 32.6 us where the median takes 25.
 //
 // P is kept to 16 bits for bf16 values (two bf16 terms): with one, its rounding is as large as that of the output itself.  8-bit keys
@@ -36,8 +36,9 @@ namespace a3 {
 constexpr int PD_WARPS = 8;      // of a CTA, one per SM
 constexpr int PD_STAGE = 8192;   // bytes of a tile: keys in the lower half, values in the upper
 constexpr float LN2 = 0.693147180559945309f;
-// A sequence (of a unit of heads) has CTAs to itself, without a second launch, where that leaves a warp PD_ALONE tiles at most; as many, up to PD_CTAS
-// in a cluster, as run at once, but no more once a warp has PD_FEW.  On the device, 32 query heads over 8, with CTAs of its own and on
+// A sequence (of a unit of heads) has CTAs to itself, without a second launch, where that leaves a warp PD_ALONE tiles at most if the page table's row is full:
+// the host does not know the lengths.  So one sequence of 600 slots takes 6.2 us behind a table of 38 pages of 16 and 8.9 behind one of 8 192, of 5 153 9.9 and
+// 11.6, 16 of 760 9.6 and 14.5 (keys in L2).  As many CTAs, up to PD_CTAS in a cluster, as run at once, but no more once a warp has PD_FEW.  On the device, 32 query heads over 8, with CTAs of its own and on
 // the line: one sequence of 600 slots 6.3 us and 9.1, 2 500 7.6 and 9.7, 5 100 9.5 and 10.3; 8 of 1 200 10.5 and 12.7; 4 of 2 500 11.5 and 13.6;
 // 16 of 760, a CTA and 6 tiles a warp each, 11.5 and 16.2; in 8 bits, whose tiles are twice the slots and the work, one of 1 200 6.9 and 10.5,
 // of 5 100 10.8 and 11.6, and of 9 000 with more than PD_ALONE_E4M3 tiles a warp 12.8 and 12.1.  With no more CTAs than PD_ALONE asks for: 600
