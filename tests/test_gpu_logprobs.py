@@ -277,7 +277,7 @@ def test_a_shift_of_all_logits_costs_no_time(eng):
             b.record()
             torch.cuda.synchronize()
             best.append(a.elapsed_time(b))
-        return sorted(best)[3]
+        return min(best)
 
     for dtype, shift, M, V in ((torch.float32, 1000.0, 1, 128256), (torch.float32, 6000.0, 300, 30000), (torch.float16, 1000.0, 300, 30000), (torch.float32, 6000.0, 64, 3000)):
         x, _ = rows(M, V, torch.float32, 12, std=2.5)
